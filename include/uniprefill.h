@@ -470,6 +470,131 @@ int uniprefill_fused_top_p_chunked(const up_params* p, const void* q, const void
                                    int32_t* pos_out, int32_t* kept_idx, int32_t* new_cu_seqlens_dev,
                                    float* scores, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- The attention layer around a drop --------------------------------------
+ *
+ * What the scoring entries are fed by (an attention layer that returns its
+ * log-sum-exp) and what the slots of uniprefill_slot_mapping point into (a paged
+ * KV cache, here in 4 bits, the decode attention over it, and its shrinking).
+ * Rows, strides, paged addressing, streams, errors and ownership as above;
+ * up_params gives num_seqs, total_tokens, the heads, head_dim, q_row_stride,
+ * k_row_stride, softmax_scale and qk_dtype (the drop layer's parameters may be
+ * handed over as they are).  Query, key and value rows must be finite where a
+ * token reads them; what lies beyond the sequences is never read into a result.
+ * Batches of more than 2^31 - 1 work items are refused (UP_ERR_UNSUPPORTED). */
+
+/* Causal attention of a packed batch (Eq. 2; "Sparsity Propagation": the layer
+ * whose queries and keys are scored): token i of sequence r, with P_r earlier
+ * tokens, sees keys 0 .. P_r + i;
+ *     out[t, h] = sum_i w_i v[i, h / (num_q_heads / num_kv_heads)],
+ *     w_i = exp(scale * <q_t, k_i>) / sum_j exp(scale * <q_t, k_j>),
+ *     lse_out[h * lse_row_stride + t] = ln sum_j exp(scale * <q_t, k_j>)
+ * -- the lse that uniprefill_fused_lse, _score_lse and _fused_top_p_lse take.
+ * Keys and values: packed like the tokens (cu_seqlens_k_dev/_host NULL), packed
+ * by cu_seqlens_k after earlier context, or in a paged cache (block_table given,
+ * values in the slots of their keys).  After a drop the compacted stream is a
+ * batch of its own (new_cu_seqlens): the order of its tokens is what is causal.
+ *   v                 like k, v_row_stride elements between tokens
+ *   out               [T, num_q_heads, head_dim] in qk_dtype, out_row_stride
+ *                     elements between tokens; only the batch's rows are written
+ *   lse_out           float, may be NULL; lse_row_stride >= total_tokens (UP_ERR_SHAPE)
+ *   workspace         from uniprefill_attention_plan (256-byte aligned): room to
+ *                     split long key ranges of few query rows; 0 bytes (and NULL)
+ *                     where the batch fills the chip by itself
+ * Products of bf16 operands are exact and summed in float; softmax statistics and
+ * sums are float; the weights are rounded to bf16 (half a step: relative 2^-8) for the product
+ * with the values.  UP_F32 operands: float throughout. */
+int uniprefill_attention_plan(const up_params* p, const int32_t* cu_seqlens_host,
+                              const int32_t* cu_seqlens_k_host, size_t* workspace_bytes);
+int uniprefill_attention(const up_params* p, const void* q, const void* k, const void* v, int64_t v_row_stride,
+                         const int32_t* cu_seqlens_dev, const int32_t* cu_seqlens_host,
+                         const int32_t* cu_seqlens_k_dev, const int32_t* cu_seqlens_k_host,
+                         const int32_t* block_table, int64_t block_table_stride, int32_t kv_block_size,
+                         void* out, int64_t out_row_stride, float* lse_out, int64_t lse_row_stride,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* The 4-bit KV cache: num_slots rows of cache_row_stride bytes for the keys and
+ * as many for the values (cache_row_stride a multiple of 16 and at least
+ * uniprefill_q4_row_bytes, else UP_ERR_ALIGN / UP_ERR_SHAPE).  A row holds one
+ * token: the codes of all kv heads, two per byte (element 2j of a head in the
+ * low half of its byte j), then for every head and 64 consecutive elements a
+ * pair of bf16 (lowest value, step).  An element stands for lowest + step * code:
+ *     lowest = the largest bf16 not above the 64 elements' minimum,
+ *     step   = the smallest bf16 not below (maximum - lowest) / 15,
+ *     code   = (element - lowest) / step rounded to the nearest whole number,
+ *              ties to even, at most 15 (0 where step is 0).
+ * uniprefill_q4_row_bytes: bytes of a row; 0 for a head_dim other than 64, 128,
+ * 256 or num_kv_heads < 1.
+ *
+ * store: rows t < n (and t < count_dev[0] when that device pointer is given; the
+ * retained count of a selection) of k [n, num_kv_heads, head_dim] (k_row_stride)
+ * and v (v_row_stride) enter the slots slots[t] (int64, as
+ * uniprefill_slot_mapping writes them).  Rows whose slot lies outside
+ * [0, num_slots) are left out (padding); no slot may be named twice.  k with
+ * k_cache, or v with v_cache, may both be NULL.
+ * load: the way back, in qk_dtype: row t of k_out / v_out receives the values
+ * that slot slots[t] stands for, rounded once; rows whose slot lies outside
+ * [0, num_slots) are left as they are. */
+int64_t uniprefill_q4_row_bytes(int32_t num_kv_heads, int32_t head_dim);
+int uniprefill_cache_store_q4(const up_params* p, const void* k, const void* v, int64_t v_row_stride,
+                              const int64_t* slots, int64_t n, const int32_t* count_dev, void* k_cache,
+                              void* v_cache, int64_t cache_row_stride, int64_t num_slots, void* stream);
+int uniprefill_cache_load_q4(const up_params* p, const void* k_cache, const void* v_cache,
+                             int64_t cache_row_stride, int64_t num_slots, const int64_t* slots, int64_t n,
+                             const int32_t* count_dev, void* k_out, void* v_out, int64_t v_row_stride,
+                             void* stream);
+
+/* One decode step over the 4-bit cache: query row r (one token of sequence r;
+ * total_tokens == num_seqs, else UP_ERR_SHAPE; qk_dtype UP_BF16, else
+ * UP_ERR_UNSUPPORTED) attends to the first kv_len_dev[r] tokens of its
+ * block-table row (one row of uniprefill_seqused; read on the device, values
+ * outside [0, max_kv_len] count as the nearer end).  max_kv_len sizes the launch
+ * and the workspace; a block-table row must hold it (UP_ERR_SHAPE).  A sequence
+ * of length 0 gets zeros and lse -inf.
+ *   out, lse_out      as for uniprefill_attention (lse_out may be NULL)
+ *   mass_out          float, may be NULL: mass_out[r * mass_row_stride + i] =
+ *                     mass_in[same] + mean over the query heads of w_i for
+ *                     i < kv_len[r] (mass_in NULL = 0; mass_in == mass_out adds
+ *                     in place); other entries are left as they are.
+ *                     mass_row_stride >= max_kv_len (UP_ERR_SHAPE)
+ *   workspace         from uniprefill_attention_q4_plan (want_mass: whether
+ *                     mass_out will be given), 256-byte aligned
+ * The codes enter the products as whole numbers and the steps in float; the
+ * weights times their steps are rounded to bf16 for the product with the values. */
+int uniprefill_attention_q4_plan(const up_params* p, int32_t max_kv_len, int32_t want_mass,
+                                 size_t* workspace_bytes);
+int uniprefill_attention_q4(const up_params* p, const void* q, const void* k_cache, const void* v_cache,
+                            int64_t cache_row_stride, const int32_t* kv_len_dev, int32_t max_kv_len,
+                            const int32_t* block_table, int64_t block_table_stride, int32_t kv_block_size,
+                            void* out, int64_t out_row_stride, float* lse_out, int64_t lse_row_stride,
+                            const float* mass_in, float* mass_out, int64_t mass_row_stride, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* Eviction from a paged cache by accumulated attention weight: of the first
+ * kv_len_dev[r] tokens of sequence r (clamped to [0, max_kv_len]) at most
+ * `budget` stay: all of them if they are no more; otherwise the first n_sink,
+ * the last n_recent, and of the others those with the largest mass, equal
+ * masses resolving to the lower index (the order of Eq. 14).  budget >= 1 and
+ * budget >= n_sink + n_recent, else UP_ERR_RANGE.  The kept tokens' rows of both
+ * caches (row_bytes of the cache_row_stride bytes of a slot; any cache whose row
+ * holds one token; v_cache may be NULL) are copied in order into the first
+ * slots of the sequence's row of new_table, and their masses into mass_out.
+ *   Out of place: the pages named by new_table must be none of those that any
+ *   sequence of the call is read from -- pages that sequences share (a common
+ *   prefix) stay intact, and freeing the old pages is the caller's.
+ *   kept_idx [num_seqs][mass_out_stride] and mass_out [num_seqs][mass_out_stride]
+ *   (mass_out_stride >= budget, UP_ERR_SHAPE): entries j < new_len[r] are written;
+ *   kept_idx is ascending.  mass must be finite.  Both block tables have rows of
+ *   kv_block_size-token pages that hold max_kv_len (block_table) and the smaller of
+ *   budget and max_kv_len (new_table) tokens, else UP_ERR_SHAPE.  row_bytes, cache_row_stride:
+ *   multiples of 16 (UP_ERR_ALIGN), row_bytes >= 16 and <= cache_row_stride. */
+int uniprefill_cache_evict(void* k_cache, void* v_cache, int64_t row_bytes, int64_t cache_row_stride,
+                           const float* mass, int64_t mass_row_stride, const int32_t* kv_len_dev,
+                           int32_t num_seqs, int32_t max_kv_len, int32_t budget, int32_t n_sink,
+                           int32_t n_recent, const int32_t* block_table, int64_t block_table_stride,
+                           const int32_t* new_table, int64_t new_table_stride, int32_t kv_block_size,
+                           int32_t* kept_idx, float* mass_out, int64_t mass_out_stride, int32_t* new_len,
+                           void* stream);
+
 /* Static, never NULL. */
 const char* uniprefill_status_string(int status);
 

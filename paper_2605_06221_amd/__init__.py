@@ -8,6 +8,8 @@ from .binding import (  # noqa: F401
     uniprefill_compact_column, uniprefill_seqused, uniprefill_score_paged, uniprefill_fused_paged, uniprefill_select_top_p_chunked,
     uniprefill_fused_top_p_chunked, uniprefill_keep_mask, uniprefill_fused_lse, uniprefill_score_lse,
     uniprefill_fused_top_p_lse, uniprefill_score_partial, uniprefill_scores_from_partials, uniprefill_plan_chunked, uniprefill_score_chunked, uniprefill_select_chunked, uniprefill_fused_chunked,
+    uniprefill_attention_plan, uniprefill_attention, uniprefill_q4_row_bytes, uniprefill_cache_store_q4,
+    uniprefill_cache_load_q4, uniprefill_attention_q4_plan, uniprefill_attention_q4, uniprefill_cache_evict,
     UP_PHASE_PLAN, UP_PHASE_ROW_STATS, UP_PHASE_MERGE_STATS, UP_PHASE_SWEEP_SELECT, UP_PHASE_GATHER,
     UP_PHASE_ALL, UP_PHASE_GATHER_IN_SELECT,
 )

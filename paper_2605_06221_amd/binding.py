@@ -28,7 +28,9 @@ EXPORTS = ["uniprefill_plan", "uniprefill_score", "uniprefill_select", "uniprefi
            "uniprefill_fused_top_p_chunked", "uniprefill_keep_mask", "uniprefill_fused_lse",
            "uniprefill_score_lse", "uniprefill_fused_top_p_lse", "uniprefill_score_partial",
            "uniprefill_scores_from_partials", "uniprefill_fused_static",
-           "uniprefill_status_string"]
+           "uniprefill_attention_plan", "uniprefill_attention", "uniprefill_q4_row_bytes", "uniprefill_cache_store_q4",
+           "uniprefill_cache_load_q4", "uniprefill_attention_q4_plan", "uniprefill_attention_q4",
+           "uniprefill_cache_evict", "uniprefill_status_string"]
 
 UP_PHASE_PLAN, UP_PHASE_ROW_STATS, UP_PHASE_MERGE_STATS, UP_PHASE_SWEEP_SELECT, UP_PHASE_GATHER = 1, 2, 4, 8, 16
 UP_PHASE_ALL = 31
@@ -98,8 +100,18 @@ def _load():
     lib.uniprefill_slot_mapping.argtypes = [i32p, i32p, i32, i32p, i64, i32, i64, vp, vp]
     lib.uniprefill_keep_mask.argtypes = [i32p, i64, i32p, i64, vp, vp]
     lib.uniprefill_seqused.argtypes = [i32p, i32, i32p, i32p, i32p, i32, i32, i32p, vp]
+    lib.uniprefill_attention_plan.argtypes = [P, i32p, i32p, ctypes.POINTER(sz)]
+    lib.uniprefill_attention.argtypes = [P, vp, vp, vp, i64, i32p, i32p] + keys + table + [vp, i64, f32p, i64] + ws + [vp]
+    lib.uniprefill_q4_row_bytes.argtypes = [i32, i32]
+    lib.uniprefill_cache_store_q4.argtypes = [P, vp, vp, i64, vp, i64, i32p, vp, vp, i64, i64, vp]
+    lib.uniprefill_cache_load_q4.argtypes = [P, vp, vp, i64, i64, vp, i64, i32p, vp, vp, i64, vp]
+    lib.uniprefill_attention_q4_plan.argtypes = [P, i32, i32, ctypes.POINTER(sz)]
+    lib.uniprefill_attention_q4.argtypes = [P, vp, vp, vp, i64, i32p, i32] + table + [vp, i64, f32p, i64, f32p, f32p, i64] + ws + [vp]
+    lib.uniprefill_cache_evict.argtypes = [vp, vp, i64, i64, f32p, i64, i32p, i32, i32, i32, i32, i32, i32p, i64, i32p, i64, i32,
+                                           i32p, f32p, i64, i32p, vp]
     for name in EXPORTS[:-1]:
         getattr(lib, name).restype = ctypes.c_int
+    lib.uniprefill_q4_row_bytes.restype = i64
     lib.uniprefill_status_string.argtypes = [ctypes.c_int]
     lib.uniprefill_status_string.restype = ctypes.c_char_p
     return lib
@@ -428,3 +440,72 @@ def uniprefill_slot_mapping(pos_kept, new_cu_seqlens_dev, num_seqs, block_table,
                                       int(block_table_stride), int(kv_block_size), int(capacity), ptr(slots),
                                       _stream(stream))
     return _check(st, "uniprefill_slot_mapping", check)
+
+
+def uniprefill_attention_plan(p: up_params, cu_seqlens_host: np.ndarray, cu_seqlens_k_host=None, *, check: bool = True):
+    """Returns (status, workspace_bytes)."""
+    ws = ctypes.c_size_t(0)
+    st = _lib.uniprefill_attention_plan(ctypes.byref(p), ptr(cu_seqlens_host), ptr(cu_seqlens_k_host), ctypes.byref(ws))
+    _check(st, "uniprefill_attention_plan", check)
+    return st, int(ws.value)
+
+
+def uniprefill_attention(p, q, k, v, v_row_stride, cu_seqlens_dev, cu_seqlens_host, cu_seqlens_k_dev, cu_seqlens_k_host,
+                         block_table, block_table_stride, kv_block_size, out, out_row_stride, lse_out, lse_row_stride,
+                         workspace, workspace_bytes, stream=None, check=True):
+    st = _lib.uniprefill_attention(ctypes.byref(p), ptr(q), ptr(k), ptr(v), int(v_row_stride), ptr(cu_seqlens_dev),
+                                   ptr(cu_seqlens_host), ptr(cu_seqlens_k_dev), ptr(cu_seqlens_k_host), ptr(block_table),
+                                   int(block_table_stride), int(kv_block_size), ptr(out), int(out_row_stride), ptr(lse_out),
+                                   int(lse_row_stride), ptr(workspace), workspace_bytes, _stream(stream))
+    return _check(st, "uniprefill_attention", check)
+
+
+def uniprefill_q4_row_bytes(num_kv_heads, head_dim):
+    return int(_lib.uniprefill_q4_row_bytes(int(num_kv_heads), int(head_dim)))
+
+
+def uniprefill_cache_store_q4(p, k, v, v_row_stride, slots, n, count_dev, k_cache, v_cache, cache_row_stride, num_slots,
+                              stream=None, check=True):
+    st = _lib.uniprefill_cache_store_q4(ctypes.byref(p), ptr(k), ptr(v), int(v_row_stride), ptr(slots), int(n),
+                                        ptr(count_dev), ptr(k_cache), ptr(v_cache), int(cache_row_stride), int(num_slots),
+                                        _stream(stream))
+    return _check(st, "uniprefill_cache_store_q4", check)
+
+
+def uniprefill_cache_load_q4(p, k_cache, v_cache, cache_row_stride, num_slots, slots, n, count_dev, k_out, v_out,
+                             v_row_stride, stream=None, check=True):
+    st = _lib.uniprefill_cache_load_q4(ctypes.byref(p), ptr(k_cache), ptr(v_cache), int(cache_row_stride), int(num_slots),
+                                       ptr(slots), int(n), ptr(count_dev), ptr(k_out), ptr(v_out), int(v_row_stride),
+                                       _stream(stream))
+    return _check(st, "uniprefill_cache_load_q4", check)
+
+
+def uniprefill_attention_q4_plan(p: up_params, max_kv_len, want_mass, *, check: bool = True):
+    """Returns (status, workspace_bytes)."""
+    ws = ctypes.c_size_t(0)
+    st = _lib.uniprefill_attention_q4_plan(ctypes.byref(p), int(max_kv_len), int(bool(want_mass)), ctypes.byref(ws))
+    _check(st, "uniprefill_attention_q4_plan", check)
+    return st, int(ws.value)
+
+
+def uniprefill_attention_q4(p, q, k_cache, v_cache, cache_row_stride, kv_len_dev, max_kv_len, block_table,
+                            block_table_stride, kv_block_size, out, out_row_stride, lse_out, lse_row_stride, mass_in,
+                            mass_out, mass_row_stride, workspace, workspace_bytes, stream=None, check=True):
+    st = _lib.uniprefill_attention_q4(ctypes.byref(p), ptr(q), ptr(k_cache), ptr(v_cache), int(cache_row_stride),
+                                      ptr(kv_len_dev), int(max_kv_len), ptr(block_table), int(block_table_stride),
+                                      int(kv_block_size), ptr(out), int(out_row_stride), ptr(lse_out), int(lse_row_stride),
+                                      ptr(mass_in), ptr(mass_out), int(mass_row_stride), ptr(workspace), workspace_bytes,
+                                      _stream(stream))
+    return _check(st, "uniprefill_attention_q4", check)
+
+
+def uniprefill_cache_evict(k_cache, v_cache, row_bytes, cache_row_stride, mass, mass_row_stride, kv_len_dev, num_seqs,
+                           max_kv_len, budget, n_sink, n_recent, block_table, block_table_stride, new_table,
+                           new_table_stride, kv_block_size, kept_idx, mass_out, mass_out_stride, new_len, stream=None,
+                           check=True):
+    st = _lib.uniprefill_cache_evict(ptr(k_cache), ptr(v_cache), int(row_bytes), int(cache_row_stride), ptr(mass),
+                                     int(mass_row_stride), ptr(kv_len_dev), int(num_seqs), int(max_kv_len), int(budget),
+                                     int(n_sink), int(n_recent), ptr(block_table), int(block_table_stride), ptr(new_table),
+                                     int(new_table_stride), int(kv_block_size), ptr(kept_idx), ptr(mass_out),
+                                     int(mass_out_stride), ptr(new_len), _stream(stream))
+    return _check(st, "uniprefill_cache_evict", check)

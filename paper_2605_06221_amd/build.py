@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libuniprefill.so")
 PIPES_BENCH_PATH = os.path.join(HERE, "up_pipes_bench.exe")
-SOURCES = ["up_api.hip", "up_copy.hip", "up_select.hip", "up_sweep.hip", "up_topp.hip"]
+SOURCES = ["up_api.hip", "up_attn.hip", "up_copy.hip", "up_evict.hip", "up_q4.hip", "up_select.hip", "up_sweep.hip", "up_topp.hip"]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",

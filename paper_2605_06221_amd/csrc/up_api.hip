@@ -920,6 +920,12 @@ int uniprefill_fused_static(const up_params* p, const void* q, const void* k, co
                     (size_t)UNIPREFILL_STATIC_SCRATCH_BYTES, UP_PHASE_ALL, stream);
 }
 
+}  // extern "C"
+
+#include "up_attn_api.h"
+
+extern "C" {
+
 const char* uniprefill_status_string(int status) {
   switch (status) {
     case UP_OK: return "ok";

@@ -1,0 +1,452 @@
+// Causal attention of a packed batch on the gfx950 matrix cores (Eq. 2's weights applied to the values), with the
+// rows' log-sum-exp.
+//
+// One pass over the keys with a running softmax: for a row with reference m (log2 units), sum l and
+// accumulator o, a tile of keys adds  l += sum_i 2^(x_i - m),  o += sum_i 2^(x_i - m) v_i  with
+// x_i = scale*log2(e)*<q, k_i>; when a tile's maximum passes m by more than 2^8 the reference moves
+// up and l, o are scaled down (any reference is exact; the margin spares most of the scalings).
+//
+// Work decomposition: a work-group is 4 waves x 32 rows.  A row is a (token, query head) pair of one kv
+// head, token-major, so the query heads that share keys share a tile and a single token is a small
+// batch too.  Keys and values pass through LDS in tiles of 64 (32 where a head row has 512 bytes), double-buffered,
+// fetched into registers while the tile before them is worked on.
+//
+// The products are formed transposed: S^T = K Q^T leaves a lane with one query row and half of the
+// tile's keys, so the softmax statistics are sums inside a lane and one exchange between lane
+// halves, and the weights already sit in the operand layout of O^T = V^T P^T: the contraction runs over
+// the keys in the order in which the lanes hold them.  V^T comes out of row-major LDS through the
+// transposing read (bf16) or plain reads (float operands).
+#include <type_traits>
+
+#include "up_attn.h"
+
+namespace up {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kAttnThreads = 256;
+constexpr float kAttnSlack = 8.0f;      // log2 units by which a weight may pass 1 before the reference moves
+
+template <bool F32, int D>
+struct AttnTile {
+  static constexpr int SRCB = D * (F32 ? 4 : 2);          // bytes of a head row
+  static constexpr int PPR = SRCB / 16;                   // 16-byte pieces of it
+  static constexpr int KT = SRCB == 512 ? 32 : 64;        // keys per tile
+  static constexpr int SUB = KT / 32;
+  static constexpr int PIECES = KT * PPR / kAttnThreads;  // pieces per thread and tile
+  static constexpr int ROWSTEP = kAttnThreads / PPR;
+  static constexpr int KREG = SRCB / 32;                  // 16-byte registers of a lane's half row
+  static constexpr int DT = D / 32;
+  static constexpr int PLACES = SRCB == 512 ? 1 : 2;      // work-groups per CU that the registers allow
+};
+
+// Rows in LDS are not padded; the 16-byte pieces of a row are permuted instead.  Keys: 16 lanes that
+// read the same piece of consecutive rows find 16 different places.  Values (bf16): the transposing
+// read takes 64 bytes of 4 consecutive rows at a time.
+template <bool F32, int D>
+__device__ __forceinline__ int k_piece(int row, int piece) {
+  constexpr int PPR = AttnTile<F32, D>::PPR;
+  return row * PPR + (piece ^ (row & (PPR < 16 ? PPR - 1 : 15)));
+}
+template <bool F32, int D>
+__device__ __forceinline__ int v_piece(int row, int piece) {
+  constexpr int PPR = AttnTile<F32, D>::PPR;
+  if (F32) return row * PPR + piece;
+  return row * PPR + (piece ^ (PPR == 8 ? (row & 2) << 1 : (row & 3) << 2));
+}
+
+__device__ __forceinline__ float attn_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// (by value: a bit cast straight from an element of a vector takes the vector's first)
+__device__ __forceinline__ float as_float(unsigned w) { return __builtin_bit_cast(float, w); }
+
+// The value of the other lane half beside the own one: v_permlane32_swap exchanges the upper half of one register
+// with the lower half of another, so of two copies one ends with the lower half's values everywhere, the other
+// with the upper half's.
+__device__ __forceinline__ f32x2 both_halves(float x) {
+  const unsigned w = __builtin_bit_cast(unsigned, x);
+  const auto r = __builtin_amdgcn_permlane32_swap(w, w, false, false);
+  return f32x2{as_float(r[0]), as_float(r[1])};
+}
+__device__ __forceinline__ float half_max(float x) {
+  const f32x2 v = both_halves(x);
+  return fmaxf(v.x, v.y);
+}
+__device__ __forceinline__ float half_sum(float x) {
+  const f32x2 v = both_halves(x);
+  return v.x + v.y;
+}
+
+__device__ __forceinline__ unsigned pack_bf16(float a, float b) {
+  const f32x2 v = {a, b};
+  return __builtin_bit_cast(unsigned, __builtin_convertvector(v, bf16x2));
+}
+
+// Largest r with its first row tile at or before `slot` (the numbering of row tiles that needs no
+// prefix sums: sequence r starts at slot cu[r] * Gq / 128 + r).
+__device__ __forceinline__ long long attn_slot_base(int cu_r, int r, int Gq) { return (long long)cu_r * Gq / kAttnRows + r; }
+
+struct AttnItem {
+  int r;
+  int tile, part;
+  long long piece;      // number of the piece in the workspace, -1: the tile is not cut
+};
+
+// Work item -> sequence, row tile, piece.  Unsplit launches number the row tiles without a prefix sum
+// (a few numbers stand for nothing); split launches walk over the sequences' counts, 256 at a time.
+template <bool SPLIT>
+__device__ __forceinline__ bool attn_locate(const AttnArgs& a, int item, AttnItem& w, long long* sm) {
+  if (!SPLIT) {
+    int lo = 0, hi = a.R - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (attn_slot_base(a.cu[mid], mid, a.Gq) <= item) lo = mid; else hi = mid - 1;
+    }
+    w.r = lo;
+    w.tile = item - (int)attn_slot_base(a.cu[lo], lo, a.Gq);
+    w.part = 0;
+    w.piece = -1;
+    const long long N = a.cu[lo + 1] - a.cu[lo];
+    return (long long)w.tile * kAttnRows < N * a.Gq;
+  }
+  // sm[0..3]: the waves' item sums, sm[4..7]: their piece sums, sm[8..9]: the answer
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  long long items_before = 0, pieces_before = 0;
+  for (int r0 = 0; r0 < a.R; r0 += kAttnThreads) {
+    const int r = r0 + tid;
+    long long ni = 0, np = 0;
+    int parts = 1;
+    if (r < a.R) {
+      const long long N = a.cu[r + 1] - a.cu[r], L = a.cu_k[r + 1] - a.cu_k[r];
+      const long long tiles = (N * a.Gq + kAttnRows - 1) / kAttnRows;
+      parts = (int)((L + a.part_keys - 1) / a.part_keys);
+      ni = tiles * parts;
+      np = parts > 1 ? ni : 0;
+    }
+    long long si = ni, sp = np;      // inclusive sums over the wave, then over the work-group
+    for (int d = 1; d < 64; d <<= 1) {
+      const long long oi = __shfl_up(si, d), op = __shfl_up(sp, d);
+      if (lane >= d) { si += oi; sp += op; }
+    }
+    if (lane == 63) { sm[wave] = si; sm[4 + wave] = sp; }
+    __syncthreads();
+    for (int w2 = 0; w2 < wave; ++w2) { si += sm[w2]; sp += sm[4 + w2]; }
+    const long long first = items_before + si - ni;
+    if (ni > 0 && item >= first && item < first + ni) {
+      sm[8] = ((long long)r << 32) | (unsigned)(item - first);
+      sm[9] = parts > 1 ? pieces_before + sp - np : -1;
+      sm[10] = parts;
+    }
+    items_before += sm[0] + sm[1] + sm[2] + sm[3];
+    pieces_before += sm[4] + sm[5] + sm[6] + sm[7];
+    __syncthreads();
+    if (item < items_before) {
+      w.r = (int)(sm[8] >> 32);
+      const int at = (int)(sm[8] & 0xffffffff), n = (int)sm[10];
+      w.tile = at / n;
+      w.part = at % n;
+      w.piece = sm[9] < 0 ? -1 : sm[9] + at;
+      return true;
+    }
+  }
+  return false;
+}
+
+template <bool F32, int D, bool PAGED, bool SPLIT>
+__global__ __launch_bounds__(kAttnThreads, (AttnTile<F32, D>::PLACES)) void k_attn(AttnArgs a) {
+  typedef AttnTile<F32, D> T;
+  __shared__ __align__(16) u32x4 sk[2][T::KT * T::PPR];
+  __shared__ __align__(16) u32x4 sv[2][T::KT * T::PPR];
+  __shared__ long long scan[11];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+  // the kv head runs fastest: with eight heads each of the eight L2s serves the tiles of one head;
+  // the last row tiles, which see the most keys, start first
+  const int kvh = blockIdx.x % a.Hkv;
+  AttnItem w;
+  if (!attn_locate<SPLIT>(a, a.items - 1 - (int)(blockIdx.x / a.Hkv), w, scan)) return;
+  const int c0 = a.cu[w.r], N = a.cu[w.r + 1] - c0;
+  const int ck0 = a.cu_k[w.r], Lk = a.cu_k[w.r + 1] - ck0;
+  const long long row0 = (long long)w.tile * kAttnRows;
+  const long long rows_left = (long long)N * a.Gq - row0;
+  const int nrow = rows_left < kAttnRows ? (int)rows_left : kAttnRows;
+  const int tok0 = (int)(row0 / a.Gq), rem0 = (int)(row0 % a.Gq);
+  const int pos0 = Lk - N + tok0;                                  // position of the first row's token
+  const int visible = pos0 + (rem0 + nrow - 1) / a.Gq + 1;         // keys that the last row sees
+  const int k_begin = SPLIT ? w.part * a.part_keys : 0;
+  const int k_end = SPLIT && a.part_keys < visible - k_begin ? k_begin + a.part_keys : visible;
+  if (SPLIT && kvh == 0 && w.part == 0 && tid == 0)
+    a.base[attn_slot_base(c0, w.r, a.Gq) + w.tile] = w.piece < 0 ? -1 : (int)w.piece;
+  if (k_begin >= visible) return;
+
+  // ---- this lane's row
+  const bool wave_live = wave * 32 < nrow;
+  const int x = imin(wave * 32 + l32, nrow - 1);                   // (rows past the end repeat the last one)
+  const int tok = (rem0 + x) / a.Gq, hh = (rem0 + x) % a.Gq;
+  const int pos = pos0 + tok;
+  const int wave_first = pos0 + (rem0 + imin(wave * 32, nrow - 1)) / a.Gq;
+  const int wave_last = pos0 + (rem0 + imin(wave * 32 + 31, nrow - 1)) / a.Gq;
+  constexpr int HOFF = F32 ? T::SRCB / 2 : 16, KSTEP = F32 ? 16 : 32;
+  u32x4 qf[T::KREG];
+  {
+    const char* src = a.q + (long long)(c0 + tok0 + tok) * a.q_stride_b + (long long)(kvh * a.Gq + hh) * T::SRCB + half * HOFF;
+#pragma unroll
+    for (int kk = 0; kk < T::KREG; ++kk) qf[kk] = *(const u32x4*)(src + kk * KSTEP);
+  }
+
+  // ---- staging: piece tid % PPR of rows tid / PPR + ROWSTEP * i of the tile; keys past the end repeat
+  // the last one (their weights are zero)
+  const int my_row = tid / T::PPR, my_piece = tid % T::PPR;
+  const char* k_head = a.k + (long long)kvh * T::SRCB + my_piece * 16;
+  const char* v_head = a.v + (long long)kvh * T::SRCB + my_piece * 16;
+  u32x4 fk[T::PIECES], fv[T::PIECES];
+  auto fetch = [&](int k0) {
+#pragma unroll
+    for (int i = 0; i < T::PIECES; ++i) {
+      const int key = imin(k0 + my_row + i * T::ROWSTEP, Lk - 1);
+      long long row;
+      if (PAGED) {
+        unsigned blk, at;
+        divmod_by((unsigned)key, (unsigned)a.kv_block, a.kv_magic, blk, at);
+        row = (long long)a.block_table[(long long)w.r * a.table_stride + blk] * a.kv_block + at;
+      } else {
+        row = (long long)ck0 + key;
+      }
+      fk[i] = *(const u32x4*)(k_head + row * a.k_stride_b);
+      fv[i] = *(const u32x4*)(v_head + row * a.v_stride_b);
+    }
+  };
+  auto stash = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < T::PIECES; ++i) {
+      const int row = my_row + i * T::ROWSTEP;
+      sk[buf][k_piece<F32, D>(row, my_piece)] = fk[i];
+      sv[buf][v_piece<F32, D>(row, my_piece)] = fv[i];
+    }
+  };
+
+  f32x16 o[T::DT];
+#pragma unroll
+  for (int dt = 0; dt < T::DT; ++dt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[dt][e] = 0.0f;
+  float m = -INFINITY, l = 0.0f;
+
+  auto tile = [&](int k0, int buf) {
+    f32x16 s[T::SUB];
+#pragma unroll
+    for (int sub = 0; sub < T::SUB; ++sub) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[sub][e] = 0.0f;
+#pragma unroll
+      for (int kk = 0; kk < T::KREG; ++kk) {
+        const u32x4 k4 = sk[buf][k_piece<F32, D>(sub * 32 + l32, F32 ? half * (T::PPR / 2) + kk : 2 * kk + half)];
+        if (F32) {
+          const u32x4 q4 = qf[kk];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[sub] = __builtin_amdgcn_mfma_f32_32x32x2f32(as_float(k4[i]), as_float(q4[i]), s[sub], 0, 0, 0);
+        } else {
+          s[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k4), __builtin_bit_cast(bf16x8, qf[kk]), s[sub], 0, 0, 0);
+        }
+      }
+    }
+    // element e of s[sub]: key k0 + 32*sub + 8*(e/4) + 4*half + e%4, row l32
+    if (k0 + T::KT - 1 > wave_first) {
+#pragma unroll
+      for (int sub = 0; sub < T::SUB; ++sub)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (k0 + sub * 32 + 8 * (e >> 2) + 4 * half + (e & 3) > pos) s[sub][e] = -INFINITY;
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int sub = 0; sub < T::SUB; ++sub)
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) mx = fmaxf(mx, fmaxf(s[sub][e], s[sub][e + 1]));
+    const float ref = half_max(mx) * a.c;
+    if (__any(ref > m + kAttnSlack)) {
+      const float up = fmaxf(m, ref);
+      const float f = m == -INFINITY ? 0.0f : attn_exp2(m - up);
+      m = up;
+      l *= f;
+#pragma unroll
+      for (int dt = 0; dt < T::DT; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[dt][e] *= f;
+    }
+    const float neg = m == -INFINITY ? 0.0f : -m;      // (a row that has seen no key yet: all weights 2^-inf)
+    float l0 = 0.0f, l1 = 0.0f;
+#pragma unroll
+    for (int sub = 0; sub < T::SUB; ++sub)
+#pragma unroll
+      for (int e = 0; e < 16; e += 2) {
+        s[sub][e] = attn_exp2(fmaf(s[sub][e], a.c, neg));
+        s[sub][e + 1] = attn_exp2(fmaf(s[sub][e + 1], a.c, neg));
+        l0 += s[sub][e];
+        l1 += s[sub][e + 1];
+      }
+    l += l0 + l1;
+    // O^T += V^T P^T.  A contraction step takes keys in the order the lanes hold their weights.
+    if (F32) {
+#pragma unroll
+      for (int sub = 0; sub < T::SUB; ++sub)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int row = sub * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
+#pragma unroll
+          for (int dt = 0; dt < T::DT; ++dt) {
+            const float v = ((const float*)&sv[buf][0])[row * D + dt * 32 + l32];
+            o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[sub][e], o[dt], 0, 0, 0);
+          }
+        }
+    } else {
+      // 16 keys per step: lane half h holds keys 4h..4h+3 and 8+4h..8+4h+3 of them.  The transposing
+      // read gives 16 lanes a column each of 4 rows x 16 columns: its lane i points at row i/4, columns 4*(i%4)..
+      const int vrow = 4 * half + ((lane >> 2) & 3);
+      const int vpc = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), vlo = (lane & 1) * 8;
+#pragma unroll
+      for (int sub = 0; sub < T::SUB; ++sub)
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+          u32x4 pw;
+          pw.x = pack_bf16(s[sub][8 * st], s[sub][8 * st + 1]);
+          pw.y = pack_bf16(s[sub][8 * st + 2], s[sub][8 * st + 3]);
+          pw.z = pack_bf16(s[sub][8 * st + 4], s[sub][8 * st + 5]);
+          pw.w = pack_bf16(s[sub][8 * st + 6], s[sub][8 * st + 7]);
+#pragma unroll
+          for (int dt = 0; dt < T::DT; ++dt) {
+            const int r0 = sub * 32 + st * 16 + vrow;
+            typedef __attribute__((address_space(3))) s16x4* lds4;
+            const s16x4 va = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)((__attribute__((address_space(3))) char*)&sv[buf][v_piece<F32, D>(r0, dt * 4 + vpc)] + vlo));
+            const s16x4 vb = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)((__attribute__((address_space(3))) char*)&sv[buf][v_piece<F32, D>(r0 + 8, dt * 4 + vpc)] + vlo));
+            u32x4 vv;
+            vv.x = __builtin_bit_cast(u32x2, va).x;
+            vv.y = __builtin_bit_cast(u32x2, va).y;
+            vv.z = __builtin_bit_cast(u32x2, vb).x;
+            vv.w = __builtin_bit_cast(u32x2, vb).y;
+            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vv), __builtin_bit_cast(bf16x8, pw), o[dt], 0, 0, 0);
+          }
+        }
+    }
+  };
+
+  fetch(k_begin);
+  stash(0);
+  __syncthreads();
+  int buf = 0;
+  for (int k0 = k_begin; k0 < k_end; k0 += T::KT, buf ^= 1) {
+    const bool more = k0 + T::KT < k_end;
+    if (more) fetch(k0 + T::KT);
+    if (wave_live && k0 <= wave_last) tile(k0, buf);
+    if (more) stash(buf ^ 1);      // (its last readers passed the barrier before this tile)
+    __syncthreads();
+  }
+
+  l = half_sum(l);
+  if (!wave_live || wave * 32 + l32 >= nrow) return;
+  const int t = c0 + tok0 + tok, h = kvh * a.Gq + hh;
+  if (SPLIT && w.piece >= 0) {
+    const long long at = (w.piece * a.Hkv + kvh) * kAttnRows + x;
+    float* dst = a.o_part + at * D;
+#pragma unroll
+    for (int dt = 0; dt < T::DT; ++dt)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *(f32x4*)(dst + dt * 32 + 8 * j + 4 * half) = f32x4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]};
+    if (half == 0) {
+      a.ml_part[2 * at] = m;
+      a.ml_part[2 * at + 1] = l;
+    }
+    return;
+  }
+  const float inv = 1.0f / l;
+  char* dst = a.out + (long long)t * a.out_stride_b + (long long)h * T::SRCB;
+#pragma unroll
+  for (int dt = 0; dt < T::DT; ++dt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int d = dt * 32 + 8 * j + 4 * half;
+      const float v0 = o[dt][4 * j] * inv, v1 = o[dt][4 * j + 1] * inv, v2 = o[dt][4 * j + 2] * inv, v3 = o[dt][4 * j + 3] * inv;
+      if (F32) *(f32x4*)(dst + d * 4) = f32x4{v0, v1, v2, v3};
+      else *(u32x2*)(dst + d * 2) = u32x2{pack_bf16(v0, v1), pack_bf16(v2, v3)};
+    }
+  if (a.lse != nullptr && half == 0) a.lse[(long long)h * a.lse_stride + t] = (m + __log2f(l)) * 0.69314718055994530942f;
+}
+
+// Joins the pieces of the row tiles that were cut: a wave per row, the pieces in order.
+template <bool F32, int D>
+__global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int kvh = blockIdx.x % a.Hkv, slot = blockIdx.x / a.Hkv;
+  int lo = 0, hi = a.R - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (attn_slot_base(a.cu[mid], mid, a.Gq) <= slot) lo = mid; else hi = mid - 1;
+  }
+  const int r = lo, c0 = a.cu[r], N = a.cu[r + 1] - c0, Lk = a.cu_k[r + 1] - a.cu_k[r];
+  const int tile = slot - (int)attn_slot_base(c0, r, a.Gq);
+  const long long row0 = (long long)tile * kAttnRows, rows_left = (long long)N * a.Gq - row0;
+  if (rows_left <= 0) return;
+  const int first = a.base[slot];
+  if (first < 0) return;
+  const int nrow = rows_left < kAttnRows ? (int)rows_left : kAttnRows;
+  const int tok0 = (int)(row0 / a.Gq), rem0 = (int)(row0 % a.Gq);
+  const int visible = Lk - N + tok0 + (rem0 + nrow - 1) / a.Gq + 1;
+  const int parts = (visible + a.part_keys - 1) / a.part_keys;      // pieces that saw a key
+  constexpr int PER = D / 64;
+  for (int x = blockIdx.y * 4 + wave; x < nrow; x += gridDim.y * 4) {
+    const long long step = (long long)a.Hkv * kAttnRows, at0 = ((long long)first * a.Hkv + kvh) * kAttnRows + x;
+    float m = -INFINITY;
+    for (int p = 0; p < parts; ++p) m = fmaxf(m, a.ml_part[2 * (at0 + p * step)]);
+    float l = 0.0f, acc[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) acc[i] = 0.0f;
+    for (int p = 0; p < parts; ++p) {
+      const long long at = at0 + p * step;
+      const float mp = a.ml_part[2 * at];
+      const float f = mp == -INFINITY ? 0.0f : attn_exp2(mp - m);
+      l = fmaf(a.ml_part[2 * at + 1], f, l);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) acc[i] = fmaf(a.o_part[at * D + lane * PER + i], f, acc[i]);
+    }
+    const int t = c0 + tok0 + (rem0 + x) / a.Gq, h = kvh * a.Gq + (rem0 + x) % a.Gq;
+    const float inv = 1.0f / l;
+    char* dst = a.out + (long long)t * a.out_stride_b + (long long)h * D * (F32 ? 4 : 2);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      if (F32) ((float*)dst)[lane * PER + i] = acc[i] * inv;
+      else ((__bf16*)dst)[lane * PER + i] = (__bf16)(acc[i] * inv);
+    }
+    if (a.lse != nullptr && lane == 0) a.lse[(long long)h * a.lse_stride + t] = (m + __log2f(l)) * 0.69314718055994530942f;
+  }
+}
+
+template <bool F32, int D, bool PAGED>
+static hipError_t launch_attn(const AttnArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)a.items * a.Hkv), block(kAttnThreads);
+  if (a.part_keys == 0) {
+    hipLaunchKernelGGL((k_attn<F32, D, PAGED, false>), grid, block, 0, s, a);
+    return hipGetLastError();
+  }
+  hipLaunchKernelGGL((k_attn<F32, D, PAGED, true>), grid, block, 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((k_attn_join<F32, D>), dim3((unsigned)a.slots * a.Hkv, 8), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_attention(const AttnArgs& a, bool f32, int D, hipStream_t s) {
+  const bool paged = a.block_table != nullptr;
+  if (f32) {
+    if (D == 64) return paged ? launch_attn<true, 64, true>(a, s) : launch_attn<true, 64, false>(a, s);
+    return paged ? launch_attn<true, 128, true>(a, s) : launch_attn<true, 128, false>(a, s);
+  }
+  if (D == 64) return paged ? launch_attn<false, 64, true>(a, s) : launch_attn<false, 64, false>(a, s);
+  if (D == 128) return paged ? launch_attn<false, 128, true>(a, s) : launch_attn<false, 128, false>(a, s);
+  return paged ? launch_attn<false, 256, true>(a, s) : launch_attn<false, 256, false>(a, s);
+}
+
+}  // namespace up
