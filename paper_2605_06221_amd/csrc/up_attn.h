@@ -8,7 +8,6 @@
 namespace up {
 
 // --- causal attention of a packed batch
-constexpr int kAttnRows = 128;      // query rows (token x query head of one kv head) per work-group
 struct AttnArgs {
   const char* q;
   const char* k;
@@ -25,6 +24,7 @@ struct AttnArgs {
   long long lse_stride;
   float c;                         // scale * log2(e)
   int R, Hq, Hkv, Gq;
+  int rows;                        // query rows (token x query head of one kv head) per work-group: 256 or 128
   int slots;                       // row tiles of all sequences (an upper bound)
   int items;                       // work-groups per kv head: row tiles, or their pieces along the keys
   int part_keys;                   // keys per work-group when the key axis is split, else 0

@@ -6,7 +6,7 @@
 // x_i = scale*log2(e)*<q, k_i>; when a tile's maximum passes m by more than 2^8 the reference moves
 // up and l, o are scaled down (any reference is exact; the margin spares most of the scalings).
 //
-// Work decomposition: a work-group is 4 waves x 32 rows.  A row is a (token, query head) pair of one kv
+// Work decomposition: a work-group is 8 (or 4) waves x 32 rows.  A row is a (token, query head) pair of one kv
 // head, token-major, so the query heads that share keys share a tile and a single token is a small
 // batch too.  Keys and values pass through LDS in tiles of 64 (32 where a head row has 512 bytes), double-buffered,
 // fetched into registers while the tile before them is worked on.
@@ -28,35 +28,41 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kAttnThreads = 256;
 constexpr float kAttnSlack = 8.0f;      // log2 units by which a weight may pass 1 before the reference moves
 
-template <bool F32, int D>
+template <bool F32, int D, int WAVES>
 struct AttnTile {
+  static constexpr int THREADS = 64 * WAVES, ROWS = 32 * WAVES;
   static constexpr int SRCB = D * (F32 ? 4 : 2);          // bytes of a head row
   static constexpr int PPR = SRCB / 16;                   // 16-byte pieces of it
   static constexpr int KT = SRCB == 512 ? 32 : 64;        // keys per tile
   static constexpr int SUB = KT / 32;
-  static constexpr int PIECES = KT * PPR / kAttnThreads;  // pieces per thread and tile
-  static constexpr int ROWSTEP = kAttnThreads / PPR;
+  static constexpr int TILES = WAVES == 8 ? 2 : 1;        // tiles staged at a time
+  static constexpr int KS = KT * TILES;
+  static constexpr int PIECES = KS * PPR / THREADS;       // pieces per thread and staging
+  static constexpr int ROWSTEP = THREADS / PPR;
   static constexpr int KREG = SRCB / 32;                  // 16-byte registers of a lane's half row
   static constexpr int DT = D / 32;
-  static constexpr int PLACES = SRCB == 512 ? 1 : 2;      // work-groups per CU that the registers allow
+  // waves per SIMD that the registers are held to
+  static constexpr int DENSE = SRCB == 128 ? 4 : SRCB == 512 && WAVES == 4 ? 1 : 2;
 };
 
-// Rows in LDS are not padded; the 16-byte pieces of a row are permuted instead.  Keys: 16 lanes that
-// read the same piece of consecutive rows find 16 different places.  Values (bf16): the transposing
+// Rows in LDS are not padded; the 16-byte pieces of a row are permuted instead (piece p sits in place p ^ swap(row)).
+// Keys: 16 lanes that read the same piece of consecutive rows find 16 different places.  Values (bf16): the transposing
 // read takes 64 bytes of 4 consecutive rows at a time.
-template <bool F32, int D>
-__device__ __forceinline__ int k_piece(int row, int piece) {
-  constexpr int PPR = AttnTile<F32, D>::PPR;
-  return row * PPR + (piece ^ (row & (PPR < 16 ? PPR - 1 : 15)));
-}
-template <bool F32, int D>
-__device__ __forceinline__ int v_piece(int row, int piece) {
-  constexpr int PPR = AttnTile<F32, D>::PPR;
-  if (F32) return row * PPR + piece;
-  return row * PPR + (piece ^ (PPR == 8 ? (row & 2) << 1 : (row & 3) << 2));
+template <int PPR>
+__device__ __forceinline__ int k_swap(int row) { return row & (PPR < 16 ? PPR - 1 : 15); }
+template <int PPR, bool F32>
+__device__ __forceinline__ int v_swap(int row) { return F32 ? 0 : PPR == 8 ? (row & 2) << 1 : (row & 3) << 2; }
+template <int PPR>
+__device__ __forceinline__ int k_place(int row, int piece) { return row * PPR + (piece ^ k_swap<PPR>(row)); }
+template <int PPR, bool F32>
+__device__ __forceinline__ int v_place(int row, int piece) { return row * PPR + (piece ^ v_swap<PPR, F32>(row)); }
+
+// 16 bytes per lane from memory into 64 consecutive places of LDS that start at dst (the same for the whole wave)
+__device__ __forceinline__ void load_to_lds(const char* src, u32x4* dst) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                   (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
 }
 
 __device__ __forceinline__ float attn_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -87,8 +93,16 @@ __device__ __forceinline__ unsigned pack_bf16(float a, float b) {
 }
 
 // Largest r with its first row tile at or before `slot` (the numbering of row tiles that needs no
-// prefix sums: sequence r starts at slot cu[r] * Gq / 128 + r).
-__device__ __forceinline__ long long attn_slot_base(int cu_r, int r, int Gq) { return (long long)cu_r * Gq / kAttnRows + r; }
+// prefix sums: sequence r starts at slot cu[r] * Gq / rows + r).
+__device__ __forceinline__ long long attn_slot_base(const AttnArgs& a, int r) { return (long long)a.cu[r] * a.Gq / a.rows + r; }
+__device__ __forceinline__ int attn_slot_sequence(const AttnArgs& a, int slot) {
+  int lo = 0, hi = a.R - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (attn_slot_base(a, mid) <= slot) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
 
 struct AttnItem {
   int r;
@@ -98,31 +112,27 @@ struct AttnItem {
 
 // Work item -> sequence, row tile, piece.  Unsplit launches number the row tiles without a prefix sum
 // (a few numbers stand for nothing); split launches walk over the sequences' counts, 256 at a time.
-template <bool SPLIT>
+template <int WAVES, bool SPLIT>
 __device__ __forceinline__ bool attn_locate(const AttnArgs& a, int item, AttnItem& w, long long* sm) {
+  constexpr int THREADS = 64 * WAVES, ROWS = 32 * WAVES;
   if (!SPLIT) {
-    int lo = 0, hi = a.R - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (attn_slot_base(a.cu[mid], mid, a.Gq) <= item) lo = mid; else hi = mid - 1;
-    }
-    w.r = lo;
-    w.tile = item - (int)attn_slot_base(a.cu[lo], lo, a.Gq);
+    w.r = attn_slot_sequence(a, item);
+    w.tile = item - (int)attn_slot_base(a, w.r);
     w.part = 0;
     w.piece = -1;
-    const long long N = a.cu[lo + 1] - a.cu[lo];
-    return (long long)w.tile * kAttnRows < N * a.Gq;
+    return (long long)w.tile * ROWS < (long long)(a.cu[w.r + 1] - a.cu[w.r]) * a.Gq;
   }
-  // sm[0..3]: the waves' item sums, sm[4..7]: their piece sums, sm[8..9]: the answer
+  // sm[0 .. WAVES): the waves' item sums, the WAVES after them: their piece sums, then the answer
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  long long* answer = sm + 2 * WAVES;
   long long items_before = 0, pieces_before = 0;
-  for (int r0 = 0; r0 < a.R; r0 += kAttnThreads) {
+  for (int r0 = 0; r0 < a.R; r0 += THREADS) {
     const int r = r0 + tid;
     long long ni = 0, np = 0;
     int parts = 1;
     if (r < a.R) {
       const long long N = a.cu[r + 1] - a.cu[r], L = a.cu_k[r + 1] - a.cu_k[r];
-      const long long tiles = (N * a.Gq + kAttnRows - 1) / kAttnRows;
+      const long long tiles = (N * a.Gq + ROWS - 1) / ROWS;
       parts = (int)((L + a.part_keys - 1) / a.part_keys);
       ni = tiles * parts;
       np = parts > 1 ? ni : 0;
@@ -132,63 +142,71 @@ __device__ __forceinline__ bool attn_locate(const AttnArgs& a, int item, AttnIte
       const long long oi = __shfl_up(si, d), op = __shfl_up(sp, d);
       if (lane >= d) { si += oi; sp += op; }
     }
-    if (lane == 63) { sm[wave] = si; sm[4 + wave] = sp; }
+    if (lane == 63) { sm[wave] = si; sm[WAVES + wave] = sp; }
     __syncthreads();
-    for (int w2 = 0; w2 < wave; ++w2) { si += sm[w2]; sp += sm[4 + w2]; }
+    long long items_here = 0, pieces_here = 0;
+    for (int w2 = 0; w2 < WAVES; ++w2) {
+      if (w2 == wave) { si += items_here; sp += pieces_here; }
+      items_here += sm[w2];
+      pieces_here += sm[WAVES + w2];
+    }
     const long long first = items_before + si - ni;
     if (ni > 0 && item >= first && item < first + ni) {
-      sm[8] = ((long long)r << 32) | (unsigned)(item - first);
-      sm[9] = parts > 1 ? pieces_before + sp - np : -1;
-      sm[10] = parts;
+      answer[0] = r;
+      answer[1] = item - first;
+      answer[2] = parts;
+      answer[3] = parts > 1 ? pieces_before + sp - np : -1;
     }
-    items_before += sm[0] + sm[1] + sm[2] + sm[3];
-    pieces_before += sm[4] + sm[5] + sm[6] + sm[7];
+    items_before += items_here;
+    pieces_before += pieces_here;
     __syncthreads();
     if (item < items_before) {
-      w.r = (int)(sm[8] >> 32);
-      const int at = (int)(sm[8] & 0xffffffff), n = (int)sm[10];
+      w.r = (int)answer[0];
+      const int at = (int)answer[1], n = (int)answer[2];
       w.tile = at / n;
       w.part = at % n;
-      w.piece = sm[9] < 0 ? -1 : sm[9] + at;
+      w.piece = answer[3] < 0 ? -1 : answer[3] + at;
       return true;
     }
   }
   return false;
 }
 
-template <bool F32, int D, bool PAGED, bool SPLIT>
-__global__ __launch_bounds__(kAttnThreads, (AttnTile<F32, D>::PLACES)) void k_attn(AttnArgs a) {
-  typedef AttnTile<F32, D> T;
-  __shared__ __align__(16) u32x4 sk[2][T::KT * T::PPR];
-  __shared__ __align__(16) u32x4 sv[2][T::KT * T::PPR];
-  __shared__ long long scan[11];
+template <bool F32, int D, int WAVES, bool PAGED, bool SPLIT>
+__global__ __launch_bounds__(64 * WAVES, (AttnTile<F32, D, WAVES>::DENSE)) void k_attn(AttnArgs a) {
+  typedef AttnTile<F32, D, WAVES> T;
+  // (two variables per buffer, not one array of buffers: the compiler then knows that a load into one and reads of
+  // another do not meet, and does not wait for the load before them)
+  __shared__ __align__(16) u32x4 sk0[T::KS * T::PPR], sk1[T::KS * T::PPR], sv0[T::KS * T::PPR], sv1[T::KS * T::PPR];
+  static_assert(sizeof(sk0) * 4 <= 160 * 1024, "LDS of one CU");
+  __shared__ long long scan[2 * WAVES + 4];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   // the kv head runs fastest: with eight heads each of the eight L2s serves the tiles of one head;
   // the last row tiles, which see the most keys, start first
   const int kvh = blockIdx.x % a.Hkv;
   AttnItem w;
-  if (!attn_locate<SPLIT>(a, a.items - 1 - (int)(blockIdx.x / a.Hkv), w, scan)) return;
+  if (!attn_locate<WAVES, SPLIT>(a, a.items - 1 - (int)(blockIdx.x / a.Hkv), w, scan)) return;
   const int c0 = a.cu[w.r], N = a.cu[w.r + 1] - c0;
   const int ck0 = a.cu_k[w.r], Lk = a.cu_k[w.r + 1] - ck0;
-  const long long row0 = (long long)w.tile * kAttnRows;
+  const long long row0 = (long long)w.tile * T::ROWS;
   const long long rows_left = (long long)N * a.Gq - row0;
-  const int nrow = rows_left < kAttnRows ? (int)rows_left : kAttnRows;
+  const int nrow = rows_left < T::ROWS ? (int)rows_left : T::ROWS;
   const int tok0 = (int)(row0 / a.Gq), rem0 = (int)(row0 % a.Gq);
   const int pos0 = Lk - N + tok0;                                  // position of the first row's token
   const int visible = pos0 + (rem0 + nrow - 1) / a.Gq + 1;         // keys that the last row sees
   const int k_begin = SPLIT ? w.part * a.part_keys : 0;
   const int k_end = SPLIT && a.part_keys < visible - k_begin ? k_begin + a.part_keys : visible;
   if (SPLIT && kvh == 0 && w.part == 0 && tid == 0)
-    a.base[attn_slot_base(c0, w.r, a.Gq) + w.tile] = w.piece < 0 ? -1 : (int)w.piece;
+    a.base[attn_slot_base(a, w.r) + w.tile] = w.piece < 0 ? -1 : (int)w.piece;
   if (k_begin >= visible) return;
 
   // ---- this lane's row
-  const bool wave_live = wave * 32 < nrow;
+  const int uwave = __builtin_amdgcn_readfirstlane(wave);           // (uniform: branches on it are scalar)
+  const bool wave_live = uwave * 32 < nrow;
   const int x = imin(wave * 32 + l32, nrow - 1);                   // (rows past the end repeat the last one)
   const int tok = (rem0 + x) / a.Gq, hh = (rem0 + x) % a.Gq;
   const int pos = pos0 + tok;
-  const int wave_first = pos0 + (rem0 + imin(wave * 32, nrow - 1)) / a.Gq;
-  const int wave_last = pos0 + (rem0 + imin(wave * 32 + 31, nrow - 1)) / a.Gq;
+  const int wave_last = pos0 + (rem0 + imin(uwave * 32 + 31, nrow - 1)) / a.Gq;
   constexpr int HOFF = F32 ? T::SRCB / 2 : 16, KSTEP = F32 ? 16 : 32;
   u32x4 qf[T::KREG];
   {
@@ -197,34 +215,44 @@ __global__ __launch_bounds__(kAttnThreads, (AttnTile<F32, D>::PLACES)) void k_at
     for (int kk = 0; kk < T::KREG; ++kk) qf[kk] = *(const u32x4*)(src + kk * KSTEP);
   }
 
-  // ---- staging: piece tid % PPR of rows tid / PPR + ROWSTEP * i of the tile; keys past the end repeat
-  // the last one (their weights are zero)
-  const int my_row = tid / T::PPR, my_piece = tid % T::PPR;
-  const char* k_head = a.k + (long long)kvh * T::SRCB + my_piece * 16;
-  const char* v_head = a.v + (long long)kvh * T::SRCB + my_piece * 16;
-  u32x4 fk[T::PIECES], fv[T::PIECES];
-  auto fetch = [&](int k0) {
+  // ---- staging, straight from memory into LDS: a wave's load writes 64 consecutive 16-byte places, WROWS rows,
+  // lane l the place l % PPR of row l / PPR; the permutation of a row's pieces is in the address that the lane reads.
+  // Keys past the end repeat the last one (their weights are zero).  Where the rows of a load lie side by side
+  // (packed keys, or pages of a multiple of 8 tokens) and before the end, its address is a scalar plus a constant per lane.
+  constexpr int WROWS = 64 / T::PPR;
+  const int lrow = lane / T::PPR, lplace = lane % T::PPR;
+  const char* k_head = a.k + (long long)kvh * T::SRCB;
+  const char* v_head = a.v + (long long)kvh * T::SRCB;
+  // (rows of 512 bytes: the rows of a lane's loads are 8 apart, and the keys' permutation has period 16)
+  const unsigned k_at[2] = {(unsigned)(lplace ^ k_swap<T::PPR>(uwave * WROWS + lrow)) * 16u,
+                            (unsigned)(lplace ^ k_swap<T::PPR>(T::ROWSTEP + uwave * WROWS + lrow)) * 16u};
+  const unsigned v_at = (unsigned)(lplace ^ v_swap<T::PPR, F32>(uwave * WROWS + lrow)) * 16u;
+  const unsigned k_lane[2] = {(unsigned)lrow * (unsigned)a.k_stride_b + k_at[0], (unsigned)lrow * (unsigned)a.k_stride_b + k_at[1]};
+  const unsigned v_lane = (unsigned)lrow * (unsigned)a.v_stride_b + v_at;
+  const bool in_runs = !PAGED || (a.kv_block & 7) == 0;
+  const int32_t* table = PAGED ? a.block_table + (long long)w.r * a.table_stride : nullptr;
+  auto row_of = [&](int key) -> long long {
+    if (!PAGED) return (long long)ck0 + key;
+    unsigned blk, at;
+    divmod_by((unsigned)key, (unsigned)a.kv_block, a.kv_magic, blk, at);
+    return (long long)table[blk] * a.kv_block + at;
+  };
+  auto stage_run = [&](int k0, u32x4* sk, u32x4* sv) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < T::PIECES; ++i) {
-      const int key = imin(k0 + my_row + i * T::ROWSTEP, Lk - 1);
-      long long row;
-      if (PAGED) {
-        unsigned blk, at;
-        divmod_by((unsigned)key, (unsigned)a.kv_block, a.kv_magic, blk, at);
-        row = (long long)a.block_table[(long long)w.r * a.table_stride + blk] * a.kv_block + at;
-      } else {
-        row = (long long)ck0 + key;
-      }
-      fk[i] = *(const u32x4*)(k_head + row * a.k_stride_b);
-      fv[i] = *(const u32x4*)(v_head + row * a.v_stride_b);
+      const int r0 = i * T::ROWSTEP + uwave * WROWS;
+      const long long row = row_of(k0 + r0);
+      load_to_lds(k_head + row * a.k_stride_b + k_lane[i & 1], sk + r0 * T::PPR);
+      load_to_lds(v_head + row * a.v_stride_b + v_lane, sv + r0 * T::PPR);
     }
   };
-  auto stash = [&](int buf) {
+  auto stage_any = [&](int k0, u32x4* sk, u32x4* sv) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < T::PIECES; ++i) {
-      const int row = my_row + i * T::ROWSTEP;
-      sk[buf][k_piece<F32, D>(row, my_piece)] = fk[i];
-      sv[buf][v_piece<F32, D>(row, my_piece)] = fv[i];
+      const int r0 = i * T::ROWSTEP + uwave * WROWS;
+      const long long row = row_of(imin(k0 + r0 + lrow, Lk - 1));
+      load_to_lds(k_head + row * a.k_stride_b + k_at[i & 1], sk + r0 * T::PPR);
+      load_to_lds(v_head + row * a.v_stride_b + v_at, sv + r0 * T::PPR);
     }
   };
 
@@ -235,7 +263,8 @@ __global__ __launch_bounds__(kAttnThreads, (AttnTile<F32, D>::PLACES)) void k_at
     for (int e = 0; e < 16; ++e) o[dt][e] = 0.0f;
   float m = -INFINITY, l = 0.0f;
 
-  auto tile = [&](int k0, int buf) {
+  // MASK: some keys of the tile come after some rows of the wave
+  auto tile = [&](auto mask_tag, int k0, const u32x4* sk, const u32x4* sv) __attribute__((always_inline)) {
     f32x16 s[T::SUB];
 #pragma unroll
     for (int sub = 0; sub < T::SUB; ++sub) {
@@ -243,7 +272,7 @@ __global__ __launch_bounds__(kAttnThreads, (AttnTile<F32, D>::PLACES)) void k_at
       for (int e = 0; e < 16; ++e) s[sub][e] = 0.0f;
 #pragma unroll
       for (int kk = 0; kk < T::KREG; ++kk) {
-        const u32x4 k4 = sk[buf][k_piece<F32, D>(sub * 32 + l32, F32 ? half * (T::PPR / 2) + kk : 2 * kk + half)];
+        const u32x4 k4 = sk[k_place<T::PPR>(sub * 32 + l32, F32 ? half * (T::PPR / 2) + kk : 2 * kk + half)];
         if (F32) {
           const u32x4 q4 = qf[kk];
 #pragma unroll
@@ -254,18 +283,23 @@ __global__ __launch_bounds__(kAttnThreads, (AttnTile<F32, D>::PLACES)) void k_at
       }
     }
     // element e of s[sub]: key k0 + 32*sub + 8*(e/4) + 4*half + e%4, row l32
-    if (k0 + T::KT - 1 > wave_first) {
+    if (decltype(mask_tag)::value) {
 #pragma unroll
       for (int sub = 0; sub < T::SUB; ++sub)
 #pragma unroll
         for (int e = 0; e < 16; ++e)
           if (k0 + sub * 32 + 8 * (e >> 2) + 4 * half + (e & 3) > pos) s[sub][e] = -INFINITY;
     }
-    float mx = -INFINITY;
+    float mx = s[0][0];
 #pragma unroll
     for (int sub = 0; sub < T::SUB; ++sub)
 #pragma unroll
-      for (int e = 0; e < 16; e += 2) mx = fmaxf(mx, fmaxf(s[sub][e], s[sub][e + 1]));
+      for (int e = 0; e < 16; e += 8) {
+        float m8 = fmaxf(fmaxf(s[sub][e], s[sub][e + 1]), s[sub][e + 2]);
+        m8 = fmaxf(fmaxf(m8, s[sub][e + 3]), s[sub][e + 4]);
+        m8 = fmaxf(fmaxf(m8, s[sub][e + 5]), s[sub][e + 6]);
+        mx = fmaxf(fmaxf(m8, s[sub][e + 7]), mx);
+      }
     const float ref = half_max(mx) * a.c;
     if (__any(ref > m + kAttnSlack)) {
       const float up = fmaxf(m, ref);
@@ -298,7 +332,7 @@ __global__ __launch_bounds__(kAttnThreads, (AttnTile<F32, D>::PLACES)) void k_at
           const int row = sub * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
 #pragma unroll
           for (int dt = 0; dt < T::DT; ++dt) {
-            const float v = ((const float*)&sv[buf][0])[row * D + dt * 32 + l32];
+            const float v = ((const float*)sv)[row * D + dt * 32 + l32];
             o[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[sub][e], o[dt], 0, 0, 0);
           }
         }
@@ -320,8 +354,8 @@ __global__ __launch_bounds__(kAttnThreads, (AttnTile<F32, D>::PLACES)) void k_at
           for (int dt = 0; dt < T::DT; ++dt) {
             const int r0 = sub * 32 + st * 16 + vrow;
             typedef __attribute__((address_space(3))) s16x4* lds4;
-            const s16x4 va = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)((__attribute__((address_space(3))) char*)&sv[buf][v_piece<F32, D>(r0, dt * 4 + vpc)] + vlo));
-            const s16x4 vb = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)((__attribute__((address_space(3))) char*)&sv[buf][v_piece<F32, D>(r0 + 8, dt * 4 + vpc)] + vlo));
+            const s16x4 va = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)((__attribute__((address_space(3))) char*)&sv[v_place<T::PPR, F32>(r0, dt * 4 + vpc)] + vlo));
+            const s16x4 vb = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)((__attribute__((address_space(3))) char*)&sv[v_place<T::PPR, F32>(r0 + 8, dt * 4 + vpc)] + vlo));
             u32x4 vv;
             vv.x = __builtin_bit_cast(u32x2, va).x;
             vv.y = __builtin_bit_cast(u32x2, va).y;
@@ -333,23 +367,51 @@ __global__ __launch_bounds__(kAttnThreads, (AttnTile<F32, D>::PLACES)) void k_at
     }
   };
 
-  fetch(k_begin);
-  stash(0);
-  __syncthreads();
-  int buf = 0;
-  for (int k0 = k_begin; k0 < k_end; k0 += T::KT, buf ^= 1) {
-    const bool more = k0 + T::KT < k_end;
-    if (more) fetch(k0 + T::KT);
-    if (wave_live && k0 <= wave_last) tile(k0, buf);
-    if (more) stash(buf ^ 1);      // (its last readers passed the barrier before this tile)
+  // Tiles that every row sees whole and whose successor lies before the end first; then the few at the
+  // end that need the masks (or, for pages of other sizes, all of them).
+  auto staged = [&]() {      // the next tile is in LDS and everyone is done with this one
+    __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0)
     __syncthreads();
+  };
+  // (tiles are staged while the ones before them are worked on; the last readers of their buffer passed a barrier)
+  constexpr int NEXT = T::KT * T::PPR;      // places of a tile in LDS
+  auto whole_tiles = [&](int k0, const u32x4* sk, const u32x4* sv) __attribute__((always_inline)) {
+    if (!wave_live) return;
+#pragma unroll
+    for (int u = 0; u < T::TILES; ++u) tile(std::false_type{}, k0 + u * T::KT, sk + u * NEXT, sv + u * NEXT);
+  };
+  auto last_tiles = [&](int k0, const u32x4* sk, const u32x4* sv) __attribute__((always_inline)) {
+    if (!wave_live) return;
+    for (int u = 0; u < T::TILES; ++u)
+      if (k0 + u * T::KT <= wave_last && k0 + u * T::KT < k_end) tile(std::true_type{}, k0 + u * T::KT, sk + u * NEXT, sv + u * NEXT);
+  };
+  stage_any(k_begin, sk0, sv0);
+  staged();
+  int k0 = k_begin;
+  const int whole = in_runs ? imin(imin(k_end, pos0 + 1), Lk - T::KS) - T::KS : k_begin - 1;
+  for (; k0 + T::KS <= whole; k0 += 2 * T::KS) {
+    stage_run(k0 + T::KS, sk1, sv1);
+    whole_tiles(k0, sk0, sv0);
+    staged();
+    stage_run(k0 + 2 * T::KS, sk0, sv0);
+    whole_tiles(k0 + T::KS, sk1, sv1);
+    staged();
+  }
+  for (; k0 < k_end; k0 += 2 * T::KS) {
+    if (k0 + T::KS < k_end) stage_any(k0 + T::KS, sk1, sv1);
+    last_tiles(k0, sk0, sv0);
+    staged();
+    if (k0 + T::KS >= k_end) break;
+    if (k0 + 2 * T::KS < k_end) stage_any(k0 + 2 * T::KS, sk0, sv0);
+    last_tiles(k0 + T::KS, sk1, sv1);
+    staged();
   }
 
   l = half_sum(l);
   if (!wave_live || wave * 32 + l32 >= nrow) return;
   const int t = c0 + tok0 + tok, h = kvh * a.Gq + hh;
   if (SPLIT && w.piece >= 0) {
-    const long long at = (w.piece * a.Hkv + kvh) * kAttnRows + x;
+    const long long at = (w.piece * a.Hkv + kvh) * T::ROWS + x;
     float* dst = a.o_part + at * D;
 #pragma unroll
     for (int dt = 0; dt < T::DT; ++dt)
@@ -381,24 +443,19 @@ template <bool F32, int D>
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int kvh = blockIdx.x % a.Hkv, slot = blockIdx.x / a.Hkv;
-  int lo = 0, hi = a.R - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (attn_slot_base(a.cu[mid], mid, a.Gq) <= slot) lo = mid; else hi = mid - 1;
-  }
-  const int r = lo, c0 = a.cu[r], N = a.cu[r + 1] - c0, Lk = a.cu_k[r + 1] - a.cu_k[r];
-  const int tile = slot - (int)attn_slot_base(c0, r, a.Gq);
-  const long long row0 = (long long)tile * kAttnRows, rows_left = (long long)N * a.Gq - row0;
+  const int r = attn_slot_sequence(a, slot), c0 = a.cu[r], N = a.cu[r + 1] - c0, Lk = a.cu_k[r + 1] - a.cu_k[r];
+  const int tile = slot - (int)attn_slot_base(a, r);
+  const long long row0 = (long long)tile * a.rows, rows_left = (long long)N * a.Gq - row0;
   if (rows_left <= 0) return;
   const int first = a.base[slot];
   if (first < 0) return;
-  const int nrow = rows_left < kAttnRows ? (int)rows_left : kAttnRows;
+  const int nrow = rows_left < a.rows ? (int)rows_left : a.rows;
   const int tok0 = (int)(row0 / a.Gq), rem0 = (int)(row0 % a.Gq);
   const int visible = Lk - N + tok0 + (rem0 + nrow - 1) / a.Gq + 1;
   const int parts = (visible + a.part_keys - 1) / a.part_keys;      // pieces that saw a key
   constexpr int PER = D / 64;
   for (int x = blockIdx.y * 4 + wave; x < nrow; x += gridDim.y * 4) {
-    const long long step = (long long)a.Hkv * kAttnRows, at0 = ((long long)first * a.Hkv + kvh) * kAttnRows + x;
+    const long long step = (long long)a.Hkv * a.rows, at0 = ((long long)first * a.Hkv + kvh) * a.rows + x;
     float m = -INFINITY;
     for (int p = 0; p < parts; ++p) m = fmaxf(m, a.ml_part[2 * (at0 + p * step)]);
     float l = 0.0f, acc[PER];
@@ -424,29 +481,29 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
   }
 }
 
-template <bool F32, int D, bool PAGED>
+template <bool F32, int D, int WAVES, bool PAGED>
 static hipError_t launch_attn(const AttnArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)a.items * a.Hkv), block(kAttnThreads);
+  const dim3 grid((unsigned)a.items * a.Hkv), block(64 * WAVES);
   if (a.part_keys == 0) {
-    hipLaunchKernelGGL((k_attn<F32, D, PAGED, false>), grid, block, 0, s, a);
+    hipLaunchKernelGGL((k_attn<F32, D, WAVES, PAGED, false>), grid, block, 0, s, a);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((k_attn<F32, D, PAGED, true>), grid, block, 0, s, a);
+  hipLaunchKernelGGL((k_attn<F32, D, WAVES, PAGED, true>), grid, block, 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((k_attn_join<F32, D>), dim3((unsigned)a.slots * a.Hkv, 8), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
+template <bool F32, int D>
+static hipError_t launch_attn_form(const AttnArgs& a, hipStream_t s) {
+  if (a.rows == 256) return a.block_table != nullptr ? launch_attn<F32, D, 8, true>(a, s) : launch_attn<F32, D, 8, false>(a, s);
+  return a.block_table != nullptr ? launch_attn<F32, D, 4, true>(a, s) : launch_attn<F32, D, 4, false>(a, s);
+}
+
 hipError_t launch_attention(const AttnArgs& a, bool f32, int D, hipStream_t s) {
-  const bool paged = a.block_table != nullptr;
-  if (f32) {
-    if (D == 64) return paged ? launch_attn<true, 64, true>(a, s) : launch_attn<true, 64, false>(a, s);
-    return paged ? launch_attn<true, 128, true>(a, s) : launch_attn<true, 128, false>(a, s);
-  }
-  if (D == 64) return paged ? launch_attn<false, 64, true>(a, s) : launch_attn<false, 64, false>(a, s);
-  if (D == 128) return paged ? launch_attn<false, 128, true>(a, s) : launch_attn<false, 128, false>(a, s);
-  return paged ? launch_attn<false, 256, true>(a, s) : launch_attn<false, 256, false>(a, s);
+  if (f32) return D == 64 ? launch_attn_form<true, 64>(a, s) : launch_attn_form<true, 128>(a, s);
+  return D == 64 ? launch_attn_form<false, 64>(a, s) : D == 128 ? launch_attn_form<false, 128>(a, s) : launch_attn_form<false, 256>(a, s);
 }
 
 }  // namespace up

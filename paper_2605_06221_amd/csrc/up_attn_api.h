@@ -10,11 +10,13 @@ namespace {
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // ---- attention of a packed batch
-// A work-group takes 128 rows (tokens x query heads of one kv head) of one sequence and walks over the
-// keys they see.  Where the rows alone leave the chip idle -- decode rows and short chunks on long
-// caches -- the keys of every row tile are cut into pieces of part_keys and the pieces joined.
+// A work-group takes 256 rows (tokens x query heads of one kv head; 8 waves) of one sequence and walks over the
+// keys they see; 128 rows (4 waves) where work-groups of 256 would be fewer than the CUs.  Where the rows alone leave
+// the chip idle all the same -- decode rows and short chunks on long caches -- the keys of every row tile are cut into
+// pieces of part_keys and the pieces joined.
 struct AttnGeometry {
-  int part_keys, parts;      // 0, 1: not split
+  int rows;
+  int part_keys, parts;      // 0, 1: not cut
   long long items;           // work-groups per kv head
   long long pieces;          // row tiles x pieces of the sequences that are cut
   long long slots;           // row tiles in the numbering that needs no prefix sums
@@ -24,34 +26,37 @@ struct AttnGeometry {
 constexpr long long kAttnMinPart = 1024;
 
 int attn_geometry(const Problem& pb, const int32_t* cu, const int32_t* ck, AttnGeometry* g) {
-  const int D = pb.head_dim;
+  const int D = pb.head_dim, row_bytes = D * (pb.qk_is_f32 ? 4 : 2);
+  *g = AttnGeometry{};
+  g->rows = 256;
   long long longest = 0, live = 0;
-  double work = 0;
   for (int r = 0; r < pb.R; ++r) {
     const long long N = cu[r + 1] - cu[r], L = ck[r + 1] - ck[r];
-    if (N == 0) continue;
-    const long long tiles = (N * pb.Gq + kAttnRows - 1) / kAttnRows;
-    live += tiles;
-    work += (double)tiles * (double)(L - N) + 0.5 * (double)(tiles + 1) * (double)N;
-    longest = L > longest ? L : longest;
+    live += (N * pb.Gq + 255) / 256;
+    if (N > 0) longest = L > longest ? L : longest;
   }
-  *g = AttnGeometry{};
+  if (live * pb.Hkv < kCUs) g->rows = 128;
+  auto tiles_of = [&](long long N) { return (N * pb.Gq + g->rows - 1) / g->rows; };
+  double work = 0;
+  for (int r = 0; r < pb.R; ++r) {
+    const long long N = cu[r + 1] - cu[r], L = ck[r + 1] - ck[r], tiles = tiles_of(N);
+    if (N > 0) work += (double)tiles * (double)(L - N) + 0.5 * (double)(tiles + 1) * (double)N;
+  }
   g->parts = 1;
-  g->slots = (long long)pb.T * pb.Gq / kAttnRows + pb.R;
+  g->slots = (long long)pb.T * pb.Gq / g->rows + pb.R;
   g->items = g->slots;
   // work-groups that the chip holds at once
-  const int places = (pb.qk_is_f32 || D == 256) ? kCUs : 2 * kCUs;
+  const int places = kCUs * (row_bytes == 512 ? 1 : row_bytes == 128 ? 1024 / g->rows / 2 : 256 / g->rows);
   const double fair = work * pb.Hkv / places;      // keys per place if all finished together
   if ((double)longest > fair && longest > kAttnMinPart) {
     const long long want = fair > (double)kAttnMinPart ? (long long)fair : kAttnMinPart;
-    const long long part = (want + 63) / 64 * 64;
+    const long long part = (want + 127) / 128 * 128;
     if (part < longest) {
       g->part_keys = (int)part;
       g->parts = (int)((longest + part - 1) / part);
       g->items = 0;
       for (int r = 0; r < pb.R; ++r) {
-        const long long N = cu[r + 1] - cu[r], L = ck[r + 1] - ck[r];
-        const long long tiles = (N * pb.Gq + kAttnRows - 1) / kAttnRows, n = (L + part - 1) / part;
+        const long long tiles = tiles_of(cu[r + 1] - cu[r]), n = (ck[r + 1] - ck[r] + part - 1) / part;
         g->items += tiles * n;
         if (n > 1) g->pieces += tiles * n;
       }
@@ -59,9 +64,9 @@ int attn_geometry(const Problem& pb, const int32_t* cu, const int32_t* ck, AttnG
       g->base_off = off;
       off = align256(off + (size_t)g->slots * sizeof(int32_t));
       g->o_off = off;
-      off = align256(off + (size_t)g->pieces * pb.Hkv * kAttnRows * D * sizeof(float));
+      off = align256(off + (size_t)g->pieces * pb.Hkv * g->rows * D * sizeof(float));
       g->ml_off = off;
-      off = align256(off + (size_t)g->pieces * pb.Hkv * kAttnRows * 2 * sizeof(float));
+      off = align256(off + (size_t)g->pieces * pb.Hkv * g->rows * 2 * sizeof(float));
       g->total = off;
     }
   }
@@ -75,6 +80,9 @@ int check_row_stride(int64_t stride, int heads, int head_dim, int elem) {
   if ((stride * elem) % 16 != 0) return UP_ERR_ALIGN;
   return UP_OK;
 }
+
+// bytes between key (value) rows up to which a work-group's offsets of a few rows stay within 32 bits
+constexpr int64_t kMaxRowStride = 1 << 27;
 
 bool aligned_to(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1u)) == 0; }
 
@@ -200,6 +208,7 @@ int uniprefill_attention(const up_params* p, const void* q, const void* k, const
   if ((st = check_row_stride(v_row_stride, pb.Hkv, pb.head_dim, e)) != UP_OK) return st;
   if ((st = check_row_stride(out_row_stride, pb.Hq, pb.head_dim, e)) != UP_OK) return st;
   if (lse_out != nullptr && lse_row_stride < pb.T) return UP_ERR_SHAPE;
+  if (pb.k_stride * e > kMaxRowStride || v_row_stride * e > kMaxRowStride) return UP_ERR_UNSUPPORTED;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return UP_ERR_ALIGN;
   if (!aligned_to(lse_out, 4) || !aligned_to(block_table, 4)) return UP_ERR_ALIGN;
   const int32_t* ck = ks.ctx ? cu_seqlens_k_host : cu_seqlens_host;
@@ -219,7 +228,7 @@ int uniprefill_attention(const up_params* p, const void* q, const void* k, const
   a.out_stride_b = out_row_stride * e; a.lse_stride = lse_row_stride;
   a.c = pb.scale * 1.44269504088896340736f;
   a.R = pb.R; a.Hq = pb.Hq; a.Hkv = pb.Hkv; a.Gq = pb.Gq;
-  a.slots = (int)g.slots; a.items = (int)g.items; a.part_keys = g.part_keys; a.parts = g.parts;
+  a.rows = g.rows; a.slots = (int)g.slots; a.items = (int)g.items; a.part_keys = g.part_keys; a.parts = g.parts;
   if (g.part_keys > 0) {
     a.base = (int32_t*)((char*)workspace + g.base_off);
     a.o_part = (float*)((char*)workspace + g.o_off);

@@ -174,6 +174,20 @@ def test_attention_with_the_keys_cut_into_pieces(lengths, earlier, hq, hkv, D, d
         b.check()
 
 
+@pytest.mark.parametrize("lengths,earlier,hq,hkv,D,dtype,page", [
+    ([2100, 1, 67], None, 32, 8, 128, BF, 0), ([1100], [333], 64, 8, 64, BF, 16), ([700, 0, 400], [50, 0, 0], 64, 8, 256, BF, 8),
+    ([1010], [129], 64, 16, 128, F32, 24), ([1010, 1], [3, 2500], 64, 16, 64, F32, 7), ([2100, 1], [0, 30000], 32, 8, 128, BF, 16),
+    ([1050, 3], [0, 9000], 64, 8, 64, BF, 0), ([1050, 2], [100, 5000], 64, 16, 256, BF, 5),
+])
+def test_attention_in_work_groups_of_256_rows(lengths, earlier, hq, hkv, D, dtype, page):
+    """Batches with at least as many tiles of 256 rows as the chip has CUs take eight waves per work-group."""
+    _say("attention, large", lengths, earlier, hq, hkv, D, dtype, page)
+    assert sum(-(-n * (hq // hkv) // 256) for n in lengths) * hkv >= 256
+    b = Batch(31, lengths, hq, hkv, D, dtype, earlier=earlier, page=page)
+    b.run()
+    b.check()
+
+
 def test_attention_strides_scale_and_no_lse():
     _say("attention: padded rows (NaN in the padding), softmax scale, no log-sum-exp")
     b = Batch(3, [100, 37], 8, 2, 128, pad=24, scale=0.3)
