@@ -37,6 +37,9 @@ struct AttnArgs {
 // --- the 4-bit KV cache
 // waves of a decode work-group, each on a kv head (D = 256: four, with twice the registers)
 constexpr UP_HD int q4_waves(int D) { return D == 256 ? 4 : 8; }
+constexpr int kQ4MaxWaveParts = 4;       // waves of a work-group that may share a kv head's keys
+// ... and waves per SIMD that its registers are held to
+constexpr UP_HD int q4_dense(int D) { return D == 64 ? 4 : D == 128 ? 2 : 1; }
 constexpr int kQ4Group = 64;        // elements that share one (lowest value, step) pair
 UP_HD long long q4_code_bytes(int heads, int D) { return (long long)heads * D / 2; }
 UP_HD long long q4_row_bytes(int heads, int D) { return q4_code_bytes(heads, D) + (long long)heads * (D / kQ4Group) * 4; }
@@ -69,12 +72,12 @@ struct Q4AttnArgs {
   unsigned kv_magic;
   float c;
   int R, Hq, Hkv, Gq, D, max_len;
-  int part_keys;                    // keys per work-group and sequence
-  int parts;                        // work-groups along the keys
-  int head_groups;                  // work-groups per sequence and piece: q4_waves kv heads each
-  int wave_parts;                   // waves of a work-group that share a kv head, each with its own keys
-  float* o_part;                    // [R][Hq][parts * wave_parts][D]
-  float* ml_part;                   // [R][Hq][parts * wave_parts] pairs
+  int groups;                       // work-groups along the keys of all sequences
+  int head_groups;                  // ... times these: q4_waves kv heads each
+  int wave_parts;                   // waves of a work-group that share a kv head, each with 64 keys of a step
+  unsigned* seq_step;               // [R + 1] first step of every sequence in the row of all steps
+  float* o_part;                    // [groups + R][wave_parts][Hq][D]
+  float* ml_part;                   // [groups + R][wave_parts][Hq] pairs
   float* lse2;                      // [R][Hq] normaliser in log2 units, for the accumulated weights
   float* logits;                    // [R][Hq][logit_stride] in log2 units
   long long logit_stride;
@@ -104,6 +107,12 @@ hipError_t launch_q4_store(const Q4CopyArgs& a, bool f32, hipStream_t s);
 hipError_t launch_q4_load(const Q4CopyArgs& a, bool f32, hipStream_t s);
 hipError_t launch_q4_attention(const Q4AttnArgs& a, hipStream_t s);
 hipError_t launch_evict(const EvictArgs& a, hipStream_t s);
+
+// An entry of a block table at an index that is the same for the whole wave.  No kernel writes a table, so it may come through the
+// scalar cache: its wait is then not one for the vector loads in flight.
+__device__ __forceinline__ int table_entry(const int32_t* table, unsigned i) {
+  return ((const __attribute__((address_space(4))) int32_t*)table)[i];
+}
 
 // x -> (x / d, x % d) with a precomputed magic = 0xFFFFFFFF / d  (x < 2^31)
 __device__ __forceinline__ void divmod_by(unsigned x, unsigned d, unsigned magic, unsigned& qo, unsigned& ro) {

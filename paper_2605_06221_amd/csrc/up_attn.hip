@@ -241,7 +241,12 @@ __global__ __launch_bounds__(64 * WAVES, (AttnTile<F32, D, WAVES>::DENSE)) void 
 #pragma unroll
     for (int i = 0; i < T::PIECES; ++i) {
       const int r0 = i * T::ROWSTEP + uwave * WROWS;
-      const long long row = row_of(k0 + r0);
+      long long row = (long long)ck0 + k0 + r0;
+      if (PAGED) {
+        unsigned blk, at;
+        divmod_by((unsigned)(k0 + r0), (unsigned)a.kv_block, a.kv_magic, blk, at);
+        row = (long long)table_entry(table, blk) * a.kv_block + at;
+      }
       load_to_lds(k_head + row * a.k_stride_b + k_lane[i & 1], sk + r0 * T::PPR);
       load_to_lds(v_head + row * a.v_stride_b + v_lane, sv + r0 * T::PPR);
     }

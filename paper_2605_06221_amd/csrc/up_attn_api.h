@@ -120,36 +120,39 @@ int q4_copy_impl(bool store, const up_params* p, const void* k, const void* v, i
 }
 
 // Decode: a work-group has eight waves (four at D = 256), each on a kv head of its own; with fewer heads than
-// waves the ones that are left share the keys of the work-group (wave_parts of them per head).  The keys are cut
-// so that a batch whose sequences all reach max_kv_len has about 4096 work-groups: with lengths known on the
-// device alone the cut cannot follow them, and pieces of a few hundred keys keep the joining cheap
-// (one float row of D + 2 per piece and head against at least 256 cached tokens).
+// waves the ones that are left share the keys of the work-group (wave_parts of them per head).  The lengths are known on the
+// device alone: the host sizes the launch to what the chip holds at once (fewer if max_kv_len leaves less to do), and the
+// kernel cuts the steps of all sequences evenly among its work-groups.
 struct Q4Geometry {
-  int part_keys, parts, wave_parts, head_groups;
+  int groups, wave_parts, head_groups;
   long long logit_stride;
-  size_t o_off, ml_off, lse2_off, logit_off, total;
+  size_t step_off, o_off, ml_off, lse2_off, logit_off, total;
 };
 
 int q4_geometry(const Problem& pb, int max_len, bool mass, Q4Geometry* g) {
   *g = Q4Geometry{};
   g->wave_parts = 1;
   const int waves = q4_waves(pb.head_dim);
-  while (2 * g->wave_parts * pb.Hkv <= waves) g->wave_parts *= 2;
+  // (as many as there are waves, and rows in LDS: 18 pieces of 16 bytes a key at D = 64, 36 beyond)
+  const long long row_places = pb.Hkv * (pb.head_dim / 32) + (pb.Hkv * (pb.head_dim / kQ4Group) * 4 + 15) / 16;
+  while (g->wave_parts < kQ4MaxWaveParts && (g->wave_parts + 1) * pb.Hkv <= waves &&
+         (g->wave_parts + 1) * row_places <= (pb.head_dim == 64 ? 18 : 36))
+    ++g->wave_parts;
   g->head_groups = (pb.Hkv + waves - 1) / waves;
-  const long long unit = 64ll * g->wave_parts;
-  long long part = ((long long)max_len * pb.R * g->head_groups + 4095) / 4096;
-  part = part < 256 ? 256 : part;
-  part = (part + unit - 1) / unit * unit;
-  g->part_keys = (int)(part < (1ll << 30) ? part : (1ll << 30));
-  g->parts = max_len > 0 ? (int)(((long long)max_len + g->part_keys - 1) / g->part_keys) : 1;
-  const size_t rows = (size_t)pb.R * pb.Hq, pieces = (size_t)g->parts * g->wave_parts;
+  const int layers = g->head_groups * ((pb.Gq + 15) / 16), places = kCUs * (pb.head_dim == 64 ? 2 : 1);
+  const long long steps = (long long)pb.R * ((max_len + 64ll * g->wave_parts - 1) / (64ll * g->wave_parts));
+  long long groups = places / layers;
+  groups = groups < 1 ? 1 : groups;
+  groups = groups < steps ? groups : steps;
+  g->groups = groups < 1 ? 1 : (int)groups;
+  const size_t rows = (size_t)pb.R * pb.Hq, pieces = ((size_t)g->groups + pb.R) * g->wave_parts * pb.Hq;
   size_t off = 0;
-  if (pieces > 1) {
-    g->o_off = off;
-    off = align256(off + rows * pieces * pb.head_dim * sizeof(float));
-    g->ml_off = off;
-    off = align256(off + rows * pieces * 2 * sizeof(float));
-  }
+  g->step_off = off;
+  off = align256(off + ((size_t)pb.R + 1) * sizeof(unsigned));
+  g->o_off = off;
+  off = align256(off + pieces * pb.head_dim * sizeof(float));
+  g->ml_off = off;
+  off = align256(off + pieces * 2 * sizeof(float));
   if (mass) {
     g->logit_stride = ((long long)max_len + 63) / 64 * 64;
     g->lse2_off = off;
@@ -158,7 +161,7 @@ int q4_geometry(const Problem& pb, int max_len, bool mass, Q4Geometry* g) {
     off = align256(off + rows * (size_t)g->logit_stride * sizeof(float));
   }
   g->total = off;
-  if (pb.R > 65535 || g->head_groups > 65535 || rows * pieces > (size_t)INT32_MAX) return UP_ERR_UNSUPPORTED;
+  if (pb.R > 65535 || layers > 65535 || steps > INT32_MAX) return UP_ERR_UNSUPPORTED;
   return UP_OK;
 }
 
@@ -282,6 +285,7 @@ int uniprefill_attention_q4(const up_params* p, const void* q, const void* k_cac
   if (pb.R > 0 && (!q || !out || !kv_len_dev || (max_kv_len > 0 && (!k_cache || !v_cache)))) return UP_ERR_NULL;
   if (mass_in != nullptr && mass_out == nullptr) return UP_ERR_NULL;
   if ((st = check_q4_cache(pb, k_cache, v_cache, cache_row_stride)) != UP_OK) return st;
+  if (cache_row_stride > kMaxRowStride) return UP_ERR_UNSUPPORTED;
   if ((st = check_row_stride(out_row_stride, pb.Hq, pb.head_dim, 2)) != UP_OK) return st;
   if (pb.R > 0 && (st = check_table(block_table, block_table_stride, kv_block_size, max_kv_len)) != UP_OK) return st;
   if (lse_out != nullptr && lse_row_stride < pb.R) return UP_ERR_SHAPE;
@@ -301,12 +305,11 @@ int uniprefill_attention_q4(const up_params* p, const void* q, const void* k_cac
   a.kv_block = kv_block_size; a.kv_magic = 0xFFFFFFFFu / (unsigned)kv_block_size;
   a.c = pb.scale * 1.44269504088896340736f;
   a.R = pb.R; a.Hq = pb.Hq; a.Hkv = pb.Hkv; a.Gq = pb.Gq; a.D = pb.head_dim; a.max_len = max_kv_len;
-  a.part_keys = g.part_keys; a.parts = g.parts; a.wave_parts = g.wave_parts; a.head_groups = g.head_groups;
+  a.groups = g.groups; a.wave_parts = g.wave_parts; a.head_groups = g.head_groups;
   char* ws = (char*)workspace;
-  if (g.parts * g.wave_parts > 1) {
-    a.o_part = (float*)(ws + g.o_off);
-    a.ml_part = (float*)(ws + g.ml_off);
-  }
+  a.seq_step = (unsigned*)(ws + g.step_off);
+  a.o_part = (float*)(ws + g.o_off);
+  a.ml_part = (float*)(ws + g.ml_off);
   if (mass_out != nullptr) {
     a.lse2 = (float*)(ws + g.lse2_off);
     a.logits = (float*)(ws + g.logit_off);

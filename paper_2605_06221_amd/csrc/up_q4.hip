@@ -140,52 +140,145 @@ __global__ __launch_bounds__(256) void k_q4_load(Q4CopyArgs a) {
 //   S^T = C_k Q^T  in v_mfma_f32_16x16x32_bf16 tiles of 16 keys x 16 query heads, one accumulator per
 //         group of 64 elements; lane = one query head and keys 16t + 4*quarter + j;
 //   O^T = C_v^T P'^T with P' = weight * step, again one operand per group.
-// Codes of eight keys sit in one word; (w >> 4i & 0x000F000F) << 3 | 0x41804180 is two bf16 numbers 16 + code
-// (0x4180 = 16.0, whose mantissa has the code's place at bits 3..6), so a pair costs two instructions and
-// the 16 goes into the lowest value: lo - 16 step.  The word order that leaves -- elements 0,4,1,5,2,6,3,7 -- is given to
-// the other operand as well.  V's codes are transposed by the 4-bit transposing read: 16 lanes point at the rows of
-// 16 keys, eight bytes each, and lane i receives column i.
+// Codes of eight keys sit in one word; a shift and (w & 0x00780078) | 0x41804180 make two bf16 numbers 16 + code
+// (0x4180 = 16.0, whose mantissa has the code's place at bits 3..6), and the 16 goes into the lowest value: lo - 16 step.
+// The order that leaves -- elements 0,4,1,5,2,6,3,7 -- is given to the other operand as well.  V's codes
+// are transposed by the 4-bit transposing read: 16 lanes point at the rows of 16 keys, eight bytes each, and lane i receives column i.
 constexpr int kQ4Wave = 64;       // keys per wave and step
 
-// two 16 + code numbers for elements e and e + 4 of a word, e = 0..3
-__device__ __forceinline__ unsigned codes_of(unsigned w, int e) {
-  const unsigned s = e == 0 ? w << 3 : (w >> (4 * e - 3));
-  return (s & 0x00780078u) | 0x41804180u;
+// Two bf16 numbers 16 + code each for elements e and e + 4 of a word.  (The mask in a scalar register and the bias in a vector
+// register: as literals they would take an instruction each.)
+struct CodeBits { unsigned mask, bias; };
+__device__ __forceinline__ CodeBits code_bits() {
+  CodeBits b;
+  asm("s_mov_b32 %0, 0x00780078" : "=s"(b.mask));
+  asm("v_mov_b32 %0, 0x41804180" : "=v"(b.bias));
+  return b;
 }
-__device__ __forceinline__ bf16x8 codes8(unsigned w) {
-  return __builtin_bit_cast(bf16x8, u32x4{codes_of(w, 0), codes_of(w, 1), codes_of(w, 2), codes_of(w, 3)});
+__device__ __forceinline__ bf16x8 codes8(unsigned w, const CodeBits& b) {
+  return __builtin_bit_cast(bf16x8, u32x4{((w << 3) & b.mask) | b.bias, ((w >> 1) & b.mask) | b.bias,
+                                          ((w >> 5) & b.mask) | b.bias, ((w >> 9) & b.mask) | b.bias});
+}
+
+// A work-group's waves take the kv heads of one stretch of keys, 64 keys per wave and step.  The rows of a step -- the codes and
+// the pairs of the work-group's heads, whole lines of memory -- go straight into LDS, all waves loading, while the step before it
+// is worked on.  (Every wave loading the pieces of its own head instead asks the first-level cache for
+// every line eight times over: 2.5 times the bytes between the caches, and 131072 cached tokens of 8 heads took 44 us.)  A row's 16-byte
+// pieces are permuted so that the transposing reads of 64 rows spread over the banks.
+template <int D> constexpr int kQ4Places = D == 64 ? 18 : 36;      // 16-byte pieces of a key and step at most (times 64 keys: LDS)
+
+// The steps of all sequences stand in a row, sequence after sequence, and are cut evenly among the work-groups: the lengths are
+// known here and not on the host, and a ragged batch keeps every CU busy to the end.  A run may cover several sequences; the
+// piece of sequence r that work-group i leaves has number i + r, which no other pair has (along the row one of the two grows).
+// Work-group 0 leaves the first step of every sequence for the kernel that joins.
+struct Q4Cut {      // total steps among at most `groups` work-groups: the first `more` of them take one step more than the others
+  unsigned groups, each, more;
+  __device__ __forceinline__ Q4Cut(unsigned total, unsigned most) {
+    groups = total < most ? total : most;      // (every one that takes part has a step)
+    each = groups > 0 ? total / groups : 0;
+    more = total - each * groups;
+  }
+  __device__ __forceinline__ unsigned first(unsigned i) const { return i * each + (i < more ? i : more); }
+  __device__ __forceinline__ unsigned owner(unsigned step) const {
+    const unsigned wide = more * (each + 1);
+    return step < wide ? step / (each + 1) : more + (step - wide) / each;
+  }
+};
+
+struct Q4Run { int r, len; unsigned from, to, seq_first; };      // steps from .. to, beginning in sequence r
+template <int THREADS>
+__device__ __forceinline__ bool q4_run(const Q4AttnArgs& a, int step_keys, unsigned* sm, Q4Run& run) {
+  constexpr int WAVES = THREADS / 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const bool notes = blockIdx.x == 0 && blockIdx.z == 0;
+  const int chunks = (a.R + THREADS - 1) / THREADS;
+  unsigned total = 0;
+  // (batches of up to THREADS sequences: one look at the lengths; more: one for the total, one for the place)
+  for (int pass = chunks > 1 ? 0 : 1; pass < 2; ++pass) {
+    unsigned before = 0;
+    for (int c = 0; c < chunks; ++c) {
+      const int r = c * THREADS + tid;
+      const int len = r < a.R ? imin(imax(a.kv_len[r], 0), a.max_len) : 0;
+      const unsigned n = (unsigned)(len + step_keys - 1) / (unsigned)step_keys;
+      unsigned sum = n;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const unsigned other = __shfl_up(sum, d);
+        if (lane >= d) sum += other;
+      }
+      if (lane == 63) sm[wave] = sum;
+      __syncthreads();
+      unsigned chunk = 0;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        if (w == wave) sum += chunk;
+        chunk += sm[w];
+      }
+      if (pass == 1) {
+        if (chunks == 1) total = chunk;
+        const unsigned at = before + sum - n;
+        const Q4Cut cut(total, gridDim.x);
+        const unsigned from = blockIdx.x < cut.groups ? cut.first(blockIdx.x) : total;
+        if (notes && r < a.R) a.seq_step[r] = at;
+        if (notes && r == a.R - 1) a.seq_step[a.R] = before + sum;
+        if (from >= at && from < at + n) {
+          sm[WAVES] = (unsigned)r;
+          sm[WAVES + 1] = at;
+          sm[WAVES + 2] = (unsigned)len;
+        }
+      }
+      before += chunk;
+      __syncthreads();
+    }
+    if (pass == 0) total = before;
+  }
+  const Q4Cut cut(total, gridDim.x);
+  if (blockIdx.x >= cut.groups) return false;
+  run.from = cut.first(blockIdx.x);
+  run.to = cut.first(blockIdx.x + 1);
+  run.r = __builtin_amdgcn_readfirstlane(sm[WAVES]);
+  run.seq_first = __builtin_amdgcn_readfirstlane(sm[WAVES + 1]);
+  run.len = __builtin_amdgcn_readfirstlane(sm[WAVES + 2]);
+  return true;
 }
 
 template <int D, bool MASS>
-__global__ __launch_bounds__(64 * q4_waves(D)) void k_q4_attn(Q4AttnArgs a) {
-  constexpr int W = q4_waves(D);
+__global__ __launch_bounds__(64 * q4_waves(D), q4_dense(D)) void k_q4_attn(Q4AttnArgs a) {
+  constexpr int W = q4_waves(D), THREADS = 64 * W;
   constexpr int NG = D / kQ4Group;          // groups per head row
-  constexpr int HB = D / 2;                 // code bytes of a head row
-  constexpr int VROW = HB + 8;              // ... and in LDS: the eight-byte columns of 64 rows spread over the banks
-  constexpr int VPIECES = HB / 16;          // 16-byte pieces of a V row
+  constexpr int HP = D / 32;                // 16-byte pieces of a head's codes
+  constexpr int SWAP = HP - 1 < 3 ? HP - 1 : 3;
   constexpr int DT = D / 16;
-  __shared__ __align__(16) unsigned char sv[W][kQ4Wave * VROW];
-  __shared__ __align__(16) f32x2 spair[W][2][NG][kQ4Wave];      // (step, offset) of every key: K's times c, V's
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, l16 = lane & 15, quarter = lane >> 4;
-  const int r = blockIdx.y;
-  const int len = imin(imax(a.kv_len[r], 0), a.max_len);
-  const bool one = a.parts * a.wave_parts == 1;      // a single piece: the output is final
+  constexpr int PLACES = kQ4Places<D>;
+  constexpr int LOADS = (2 * PLACES + W - 1) / W;      // loads of a wave per step
+  // (two variables per buffer: see the attention of packed batches)
+  __shared__ __align__(16) u32x4 k0s[64 * PLACES], k1s[64 * PLACES], v0s[64 * PLACES], v1s[64 * PLACES];
+  __shared__ __align__(16) f32x2 spair[W][NG][kQ4Wave];      // (step, offset) of a wave's keys: K's times c, then V's
+  __shared__ long long rows0[kQ4Wave * kQ4MaxWaveParts], rows1[kQ4Wave * kQ4MaxWaveParts];      // byte offsets of a step's keys
+  static_assert(kQ4Wave * kQ4MaxWaveParts <= THREADS, "a thread per key of a step");
+  const int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l16 = lane & 15, quarter = lane >> 4;
   const int qtiles = (a.Gq + 15) / 16;
   const int q16 = (int)(blockIdx.z % qtiles) * 16;   // first query head of the group that this work-group takes
-  const int head = a.wave_parts > 1 ? wave / a.wave_parts : (int)(blockIdx.z / qtiles) * W + wave;
-  const int wp = wave % a.wave_parts;
-  if (head >= a.Hkv) return;
-  const int wkeys = a.part_keys / a.wave_parts;
-  const long long begin = (long long)blockIdx.x * a.part_keys + (long long)wp * wkeys;
-  if (begin >= len && !(one && len == 0)) return;
-  const int k_begin = (int)begin, k_end = len - k_begin < wkeys ? len : k_begin + wkeys;
+  const int head0 = a.wave_parts > 1 ? 0 : (int)(blockIdx.z / qtiles) * W;
+  const int heads = a.wave_parts > 1 ? a.Hkv : imin(W, a.Hkv - head0);
+  const int hw = wave / a.wave_parts, wp = wave % a.wave_parts;
+  const int head = head0 + hw;
+  const bool works = hw < heads;
+  const CodeBits bits = code_bits();
+  const int step_keys = kQ4Wave * a.wave_parts;
 
-  // ---- queries: lane = query head q16 + l16, element order of the codes
+  // ---- this work-group's run of steps
+  Q4Run run;
+  if (!q4_run<THREADS>(a, step_keys, (unsigned*)rows1, run)) return;
+  int r = run.r;
+
   u32x4 qf[NG][2];
   float qsum[NG];
-  const bool live = q16 + l16 < a.Gq;
-  {
-    const char* src = a.q + (long long)r * a.q_stride_b + (long long)(head * a.Gq + imin(q16 + l16, a.Gq - 1)) * (D * 2);
+  const bool live = works && q16 + l16 < a.Gq;
+  // queries of sequence r: lane = query head q16 + l16, element order of the codes
+  auto load_queries = [&]() __attribute__((always_inline)) {
+    const char* src = a.q + (long long)r * a.q_stride_b + (long long)(imin(head, a.Hkv - 1) * a.Gq + imin(q16 + l16, a.Gq - 1)) * (D * 2);
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       float sum = 0.0f;
@@ -202,74 +295,70 @@ __global__ __launch_bounds__(64 * q4_waves(D)) void k_q4_attn(Q4AttnArgs a) {
       sum += __shfl_xor(sum, 32);
       qsum[g] = sum;
     }
+  };
+
+  f32x4 o[DT], ow[NG];                          // weighted codes; sums of the rounded weights * steps (every row of it the same)
+  float m, l, ol[NG];                           // reference, sum of weights, sum of weights * offsets
+  int len = 0, first = 0, last = 0;             // the sequence's length; its keys that this work-group takes
+
+  // ---- staging.  A row in LDS: the codes of the work-group's heads (permuted pieces), then their pairs.  Load i of this wave
+  // writes 64 consecutive pieces; where its lane's piece comes from inside which row does not change from step to step
+  const int code_places = heads * HP, places = code_places + (heads * NG * 4 + 15) / 16;
+  const int loads = a.wave_parts * places;      // per cache
+  const unsigned places_magic = 0xFFFFFFFFu / (unsigned)places;
+  int from_row[LOADS], from_at[LOADS];
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int j = i * W + wave, p = (j >= loads ? j - loads : j) * 64 + lane;
+    unsigned row, place;
+    divmod_by((unsigned)p, (unsigned)places, places_magic, row, place);
+    from_row[i] = (int)row;
+    from_at[i] = (int)place < code_places ? head0 * (D / 2) + (int)(place ^ ((row >> 2) & SWAP)) * 16
+                                     : (int)q4_code_bytes(a.Hkv, D) + head0 * NG * 4 + ((int)place - code_places) * 16;
   }
-
-  f32x4 o[DT];
-  float m = -INFINITY, l = 0.0f, ol[NG];      // reference, sum of weights, what the groups' offsets add up to
+  auto stage = [&](const long long* rows, u32x4* sk, u32x4* sv) __attribute__((always_inline)) {
 #pragma unroll
-  for (int g = 0; g < NG; ++g) ol[g] = 0.0f;
-#pragma unroll
-  for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-
-  const long long head_codes = (long long)head * HB, head_pairs = q4_code_bytes(a.Hkv, D) + (long long)head * NG * 4;
-  // slot of this lane's key of the step at k0 (keys past the end repeat the last one)
-  auto slot_of = [&](int k0) -> int64_t {
+    for (int i = 0; i < LOADS; ++i) {
+      const int j = i * W + wave;
+      if (j < 2 * loads) {
+        const char* src = (j >= loads ? a.v : a.k) + rows[from_row[i]] + from_at[i];
+        u32x4* dst = j >= loads ? sv + (j - loads) * 64 : sk + j * 64;
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+      }
+    }
+  };
+  // byte offset of this thread's key of the step at k0 (keys past the end repeat the last one)
+  auto row_offset = [&](int k0) __attribute__((always_inline)) -> long long {
     unsigned blk, at;
-    divmod_by((unsigned)imin(k0 + lane, len - 1), (unsigned)a.kv_block, a.kv_magic, blk, at);
-    return (int64_t)a.block_table[(long long)r * a.table_stride + blk] * a.kv_block + at;
-  };
-  u32x2 kc[4][NG];                     // K codes: key 16t + l16, elements 64g + 16*quarter ..
-  u32x4 vc[VPIECES];                   // V codes: 16-byte pieces of keys in row order
-  unsigned kp[NG], vp[NG];             // this lane's key's pairs
-  auto fetch = [&](int64_t slot) {
-    const int lo = (int)slot, hi = (int)(slot >> 32);
-    auto of = [&](int key) { return ((int64_t)__shfl(hi, key) << 32) | (unsigned)__shfl(lo, key); };
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const char* row = a.k + of(16 * t + l16) * a.cache_stride + head_codes + quarter * 8;
-#pragma unroll
-      for (int g = 0; g < NG; ++g) kc[t][g] = *(const u32x2*)(row + g * 32);
-    }
-#pragma unroll
-    for (int i = 0; i < VPIECES; ++i) {
-      const int piece = i * 64 + lane;
-      vc[i] = *(const u32x4*)(a.v + of(piece / VPIECES) * a.cache_stride + head_codes + (piece % VPIECES) * 16);
-    }
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      kp[g] = *(const unsigned*)(a.k + slot * a.cache_stride + head_pairs + g * 4);
-      vp[g] = *(const unsigned*)(a.v + slot * a.cache_stride + head_pairs + g * 4);
-    }
+    divmod_by((unsigned)imin(k0 + tid, len - 1), (unsigned)a.kv_block, a.kv_magic, blk, at);
+    return ((long long)a.block_table[(long long)r * a.table_stride + blk] * a.kv_block + at) * a.cache_stride;
   };
 
-  if (k_begin < k_end) fetch(slot_of(k_begin));
-  for (int k0 = k_begin; k0 < k_end; k0 += kQ4Wave) {
-    // ---- V codes and the pairs into the wave's own LDS
-#pragma unroll
-    for (int i = 0; i < VPIECES; ++i) {
-      const int piece = i * 64 + lane;
-      u32x2* dst = (u32x2*)&sv[wave][(piece / VPIECES) * VROW + (piece % VPIECES) * 16];
-      dst[0] = u32x2{vc[i].x, vc[i].y};
-      dst[1] = u32x2{vc[i].z, vc[i].w};
-    }
+  // ---- one step: this wave's 64 keys from ks on, in LDS
+  auto step = [&](int ks, const u32x4* sk, const u32x4* sv) __attribute__((always_inline)) {
+    if (!works || ks >= last) return;
+    const int row0 = wp * kQ4Wave;
+    auto pair_of = [&](const u32x4* buf, int g) { return ((const unsigned*)(buf + (row0 + lane) * places + code_places))[hw * NG + g]; };
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      const float step = bf16_hi(kp[g]) * a.c;
-      spair[wave][0][g][lane] = f32x2{step, fmaf(-16.0f, step, bf16_lo(kp[g]) * a.c)};
-      spair[wave][1][g][lane] = f32x2{bf16_hi(vp[g]), fmaf(8.0f, bf16_hi(vp[g]), bf16_lo(vp[g]))};
+      const unsigned w = pair_of(sk, g);
+      const float st = bf16_hi(w) * a.c;
+      spair[wave][g][lane] = f32x2{st, fmaf(-16.0f, st, bf16_lo(w) * a.c)};
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    // ---- logits in log2 units: x[t][j] of key k0 + 16t + 4*quarter + j
+    // ---- logits in log2 units: x[t][j] of key ks + 16t + 4*quarter + j
     float x[4][4];
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
+      const int row = row0 + 16 * t + l16;
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
+        const u32x2 kc = ((const u32x2*)(sk + row * places + ((hw * HP + 2 * g + (quarter >> 1)) ^ ((row >> 2) & SWAP))))[quarter & 1];
         f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes8(kc[t][g].x), __builtin_bit_cast(bf16x8, qf[g][0]), acc, 0, 0, 0);
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes8(kc[t][g].y), __builtin_bit_cast(bf16x8, qf[g][1]), acc, 0, 0, 0);
-        const f32x4* pr = (const f32x4*)&spair[wave][0][g][16 * t + 4 * quarter];
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes8(kc.x, bits), __builtin_bit_cast(bf16x8, qf[g][0]), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes8(kc.y, bits), __builtin_bit_cast(bf16x8, qf[g][1]), acc, 0, 0, 0);
+        const f32x4* pr = (const f32x4*)&spair[wave][g][16 * t + 4 * quarter];
         const f32x4 p01 = pr[0], p23 = pr[1];
         const float add = qsum[g];
         x[t][0] = fmaf(p01.x, acc[0], g == 0 ? p01.y * add : fmaf(p01.y, add, x[t][0]));
@@ -279,25 +368,33 @@ __global__ __launch_bounds__(64 * q4_waves(D)) void k_q4_attn(Q4AttnArgs a) {
       }
       __builtin_amdgcn_sched_barrier(0);      // (keeps the registers of one tile's codes from living beside the next's)
     }
-    if (k0 + kQ4Wave < k_end) fetch(slot_of(k0 + kQ4Wave));
     if (MASS && live) {
-      float* dst = a.logits + ((long long)r * a.Hq + head * a.Gq + q16 + l16) * a.logit_stride + k0 + 4 * quarter;
+      float* dst = a.logits + ((long long)r * a.Hq + head * a.Gq + q16 + l16) * a.logit_stride + ks + 4 * quarter;
 #pragma unroll
       for (int t = 0; t < 4; ++t) *(f32x4*)(dst + 16 * t) = f32x4{x[t][0], x[t][1], x[t][2], x[t][3]};
     }
-    if (k0 + kQ4Wave > k_end) {
+    if (ks + kQ4Wave > last) {
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (k0 + 16 * t + 4 * quarter + j >= len) x[t][j] = -INFINITY;
+          if (ks + 16 * t + 4 * quarter + j >= len) x[t][j] = -INFINITY;
     }
+    // V's offset stands for code 8, the middle: what a weight's rounding multiplies is then code - 8 (24 = 16 + 8 times the rounded
+    // weights are taken back at the end), and not the lowest value or code + 16
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const unsigned w = pair_of(sv, g);
+      spair[wave][g][lane] = f32x2{bf16_hi(w), fmaf(8.0f, bf16_hi(w), bf16_lo(w))};
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
     // ---- running softmax (the first key of a step is always there: no row without a maximum)
     float mx = x[0][0];
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) mx = fmaxf(mx, x[t][j]);
+      for (int j = 0; j < 4; j += 2) mx = fmaxf(fmaxf(mx, x[t][j]), x[t][j + 1]);
     mx = fmaxf(mx, __shfl_xor(mx, 16));
     mx = fmaxf(mx, __shfl_xor(mx, 32));
     if (__any(mx > m)) {
@@ -305,7 +402,11 @@ __global__ __launch_bounds__(64 * q4_waves(D)) void k_q4_attn(Q4AttnArgs a) {
       m = up;
       l *= f;
 #pragma unroll
-      for (int g = 0; g < NG; ++g) ol[g] *= f;
+      for (int g = 0; g < NG; ++g) {
+        ol[g] *= f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ow[g][j] *= f;
+      }
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -319,13 +420,15 @@ __global__ __launch_bounds__(64 * q4_waves(D)) void k_q4_attn(Q4AttnArgs a) {
         l += x[t][j];
       }
     // ---- values.  Word 0 of a transposed read: keys 4*quarter + j of tiles 0 and 1, word 1: of tiles 2 and 3
+    const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+    const int vrow = row0 + 16 * (l16 >> 2) + 4 * quarter + (l16 & 3);
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       bf16x8 pw[2];
 #pragma unroll
       for (int mm = 0; mm < 2; ++mm) {
-        const f32x4* pa = (const f32x4*)&spair[wave][1][g][32 * mm + 4 * quarter];
-        const f32x4* pb = (const f32x4*)&spair[wave][1][g][32 * mm + 16 + 4 * quarter];
+        const f32x4* pa = (const f32x4*)&spair[wave][g][32 * mm + 4 * quarter];
+        const f32x4* pb = (const f32x4*)&spair[wave][g][32 * mm + 16 + 4 * quarter];
         const f32x4 a01 = pa[0], a23 = pa[1], b01 = pb[0], b23 = pb[1];
         const float sa[4] = {a01.x, a01.z, a23.x, a23.z}, la[4] = {a01.y, a01.w, a23.y, a23.w};
         const float sb[4] = {b01.x, b01.z, b23.x, b23.z}, lb[4] = {b01.y, b01.w, b23.y, b23.w};
@@ -334,96 +437,179 @@ __global__ __launch_bounds__(64 * q4_waves(D)) void k_q4_attn(Q4AttnArgs a) {
         for (int j = 0; j < 4; ++j) {
           const float wa = x[2 * mm][j], wb = x[2 * mm + 1][j];
           w[j] = pack2(wa * sa[j], wb * sb[j]);
-          // 24 = the 16 of every code and its middle 8 are taken back with the rounded weights that multiplied them, the
-          // middle is added with the exact ones: what a weight's rounding multiplies is code - 8, not code + 16
           ol[g] = fmaf(wa, la[j], fmaf(wb, lb[j], ol[g]));
-          ol[g] = fmaf(-24.0f, bf16_lo(w[j]) + bf16_hi(w[j]), ol[g]);
         }
         pw[mm] = __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
+        ow[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, pw[mm], ow[g], 0, 0, 0);
       }
 #pragma unroll
       for (int dd = 0; dd < 4; ++dd) {
         const int dt = g * 4 + dd;
         typedef int i32x2 __attribute__((ext_vector_type(2)));
         typedef __attribute__((address_space(3))) i32x2* lds2;
-        const int row = 16 * (l16 >> 2) + 4 * quarter + (l16 & 3);
-        const i32x2 vt = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds2)&sv[wave][row * VROW + dt * 8]);
-        o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes8((unsigned)vt.x), pw[0], o[dt], 0, 0, 0);
-        o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes8((unsigned)vt.y), pw[1], o[dt], 0, 0, 0);
+        const u32x4* at = sv + vrow * places + ((hw * HP + (dt >> 1)) ^ ((vrow >> 2) & SWAP));
+        const i32x2 vt = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds2)((__attribute__((address_space(3))) char*)at + (dt & 1) * 8));
+        o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes8((unsigned)vt.x, bits), pw[0], o[dt], 0, 0, 0);
+        o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes8((unsigned)vt.y, bits), pw[1], o[dt], 0, 0, 0);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
-  }
+  };
 
-  // ---- o[dt][j]: element 16*dt + 4*quarter + j of query head q16 + l16
-  l += __shfl_xor(l, 16);
-  l += __shfl_xor(l, 32);
+  // ---- the row offsets run two steps ahead, the rows one
+  const bool looks = tid < step_keys;
+  auto staged = [&]() __attribute__((always_inline)) {
+    __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0)
+    __syncthreads();
+  };
+  len = run.len;
+  while (true) {
+    const int seq_steps = (len + step_keys - 1) / step_keys;
+    const int here = (int)(run.from - run.seq_first), n = imin((int)(run.to - run.from), seq_steps - here);
+    const bool whole = n == seq_steps;        // the sequence is all here: the output is final
+    first = here * step_keys;
+    last = n == seq_steps - here ? len : first + n * step_keys;
+    load_queries();
+    m = -INFINITY;
+    l = 0.0f;
 #pragma unroll
-  for (int g = 0; g < NG; ++g) {
-    ol[g] += __shfl_xor(ol[g], 16);
-    ol[g] += __shfl_xor(ol[g], 32);
-  }
-  if (!live) return;
-  const long long hq = head * a.Gq + q16 + l16;
-  if (!one) {
-    const long long at = ((long long)r * a.Hq + hq) * (a.parts * a.wave_parts) + blockIdx.x * a.wave_parts + wp;
+    for (int g = 0; g < NG; ++g) { ol[g] = 0.0f; ow[g] = f32x4{0.0f, 0.0f, 0.0f, 0.0f}; }
 #pragma unroll
-    for (int dt = 0; dt < DT; ++dt) {
-      const float b = ol[dt / 4];
-      *(f32x4*)(a.o_part + at * D + dt * 16 + quarter * 4) = f32x4{o[dt][0] + b, o[dt][1] + b, o[dt][2] + b, o[dt][3] + b};
+    for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    long long at0 = 0, at1 = 0;
+    if (looks) {
+      at0 = row_offset(first);
+      at1 = row_offset(imin(first + step_keys, last - 1));
     }
-    if (quarter == 0) {
-      a.ml_part[2 * at] = m;
-      a.ml_part[2 * at + 1] = l;
+    __syncthreads();      // (rows1 held the run)
+    if (looks) {
+      rows0[tid] = at0;
+      rows1[tid] = at1;
     }
-    return;
-  }
-  const float inv = len > 0 ? 1.0f / l : 0.0f;
-  char* dst = a.out + (long long)r * a.out_stride_b + hq * (D * 2);
+    __syncthreads();
+    stage(rows0, k0s, v0s);
+    staged();
+    for (int ks = first; ks < last; ks += 2 * step_keys) {
+      long long ahead = 0;
+      if (looks) ahead = row_offset(imin(ks + 2 * step_keys, last - 1));
+      if (ks + step_keys < last) stage(rows1, k1s, v1s);
+      step(ks + wp * kQ4Wave, k0s, v0s);
+      if (looks) rows0[tid] = ahead;
+      staged();
+      if (ks + step_keys >= last) break;
+      if (looks) ahead = row_offset(imin(ks + 3 * step_keys, last - 1));
+      if (ks + 2 * step_keys < last) stage(rows0, k0s, v0s);
+      step(ks + step_keys + wp * kQ4Wave, k1s, v1s);
+      if (looks) rows1[tid] = ahead;
+      staged();
+    }
+
+    // ---- o[dt][j]: element 16*dt + 4*quarter + j of query head q16 + l16
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
 #pragma unroll
-  for (int dt = 0; dt < DT; ++dt) {
-    const float b = ol[dt / 4];
-    *(u32x2*)(dst + (dt * 16 + quarter * 4) * 2) =
-        u32x2{pack2((o[dt][0] + b) * inv, (o[dt][1] + b) * inv), pack2((o[dt][2] + b) * inv, (o[dt][3] + b) * inv)};
+    for (int g = 0; g < NG; ++g) {
+      ol[g] += __shfl_xor(ol[g], 16);
+      ol[g] += __shfl_xor(ol[g], 32);
+      ol[g] = fmaf(-24.0f, ow[g][0], ol[g]);
+    }
+    const long long hq = head * a.Gq + q16 + l16;
+    if (live && whole && a.wave_parts == 1) {
+      const float inv = 1.0f / l;
+      char* dst = a.out + (long long)r * a.out_stride_b + hq * (D * 2);
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const float b = ol[dt / 4];
+        *(u32x2*)(dst + (dt * 16 + quarter * 4) * 2) =
+            u32x2{pack2((o[dt][0] + b) * inv, (o[dt][1] + b) * inv), pack2((o[dt][2] + b) * inv, (o[dt][3] + b) * inv)};
+      }
+      const float lse2 = m + __log2f(l);
+      if (quarter == 0 && a.lse != nullptr) a.lse[hq * a.lse_stride + r] = lse2 * 0.69314718055994530942f;
+      if (quarter == 0 && MASS) a.lse2[(long long)r * a.Hq + hq] = lse2;
+    } else if (live) {
+      // (a wave without a key: reference -inf, sums 0)
+      const long long at = (((long long)blockIdx.x + r) * a.wave_parts + wp) * a.Hq + hq;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) {
+        const float b = ol[dt / 4];
+        *(f32x4*)(a.o_part + at * D + dt * 16 + quarter * 4) = f32x4{o[dt][0] + b, o[dt][1] + b, o[dt][2] + b, o[dt][3] + b};
+      }
+      if (quarter == 0) {
+        a.ml_part[2 * at] = m;
+        a.ml_part[2 * at + 1] = l;
+      }
+    }
+    run.from += n;
+    if (run.from >= run.to) return;
+    run.seq_first += seq_steps;
+    do len = imin(a.kv_len[++r], a.max_len); while (len <= 0);      // (the run goes on: a sequence with keys follows)
   }
-  const float lse2 = len > 0 ? m + __log2f(l) : -INFINITY;
-  if (quarter == 0 && a.lse != nullptr) a.lse[hq * a.lse_stride + r] = lse2 * 0.69314718055994530942f;
-  if (quarter == 0 && MASS) a.lse2[(long long)r * a.Hq + hq] = lse2;
 }
 
-// Joins a query head's pieces in order: a wave per (sequence, query head).
+// Joins the pieces of one query head of one sequence: the work-group's waves take the pieces in turn, eight in flight each, and
+// their sums are added in order.
+constexpr int kQ4JoinWaves = 16;
 template <int D>
-__global__ __launch_bounds__(256) void k_q4_join(Q4AttnArgs a) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int r = blockIdx.y, hq = blockIdx.x * 4 + wave;
-  if (hq >= a.Hq) return;
-  const int len = imin(imax(a.kv_len[r], 0), a.max_len);
-  const int pieces = a.parts * a.wave_parts, wkeys = a.part_keys / a.wave_parts;
-  const int live = (len + wkeys - 1) / wkeys;      // pieces hold consecutive runs of keys
-  constexpr int PER = D / 64;
-  const long long at0 = ((long long)r * a.Hq + hq) * pieces;
+__global__ __launch_bounds__(64 * kQ4JoinWaves) void k_q4_join(Q4AttnArgs a) {
+  constexpr int PER = D / 64, FLY = 8;
+  __shared__ float sacc[kQ4JoinWaves][D], sl[kQ4JoinWaves], sm[kQ4JoinWaves];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, waves = blockDim.x >> 6;
+  const int r = blockIdx.y, hq = blockIdx.x;
+  // steps p0 .. p1 of the row belong to this sequence, and the work-groups from i0 to i1 took them (see q4_run)
+  const unsigned p0s = a.seq_step[r], p1s = a.seq_step[r + 1];
+  const bool empty = p0s == p1s;
+  const Q4Cut cut(a.seq_step[a.R], (unsigned)a.groups);
+  const int i0 = empty ? 0 : (int)cut.owner(p0s), i1 = empty ? -1 : (int)cut.owner(p1s - 1);
+  if (i0 == i1 && a.wave_parts == 1) return;      // the one that took it all has written the output
+  const int live = (i1 - i0 + 1) * a.wave_parts;
+  const long long at0 = ((long long)i0 + r) * a.wave_parts * a.Hq + hq;
   float m = -INFINITY;
-  for (int p = lane; p < live; p += 64) m = fmaxf(m, a.ml_part[2 * (at0 + p)]);
+  for (int p = threadIdx.x; p < live; p += blockDim.x) m = fmaxf(m, a.ml_part[2 * (at0 + (long long)p * a.Hq)]);
+#pragma unroll
   for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+  if (lane == 0) sm[wave] = m;
+  __syncthreads();
+  m = sm[0];
+  for (int w = 1; w < waves; ++w) m = fmaxf(m, sm[w]);
   float l = 0.0f, acc[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) acc[i] = 0.0f;
-  for (int p = 0; p < live; ++p) {
-    const long long at = at0 + p;
-    const float f = exp2_of(a.ml_part[2 * at] - m);
-    l = fmaf(a.ml_part[2 * at + 1], f, l);
+  for (int p0 = wave; p0 < live; p0 += waves * FLY) {
+    float pm[FLY], pl[FLY], po[FLY][PER];
 #pragma unroll
-    for (int i = 0; i < PER; ++i) acc[i] = fmaf(a.o_part[at * D + lane * PER + i], f, acc[i]);
+    for (int u = 0; u < FLY; ++u) {
+      const long long at = at0 + (long long)imin(p0 + waves * u, live - 1) * a.Hq;
+      pm[u] = a.ml_part[2 * at];
+      pl[u] = a.ml_part[2 * at + 1];
+#pragma unroll
+      for (int i = 0; i < PER; ++i) po[u][i] = a.o_part[at * D + i * 64 + lane];
+    }
+#pragma unroll
+    for (int u = 0; u < FLY; ++u) {
+      const float f = p0 + waves * u < live ? exp2_of(pm[u] - m) : 0.0f;
+      l = fmaf(pl[u], f, l);
+#pragma unroll
+      for (int i = 0; i < PER; ++i) acc[i] = fmaf(po[u][i], f, acc[i]);
+    }
   }
-  const float inv = len > 0 ? 1.0f / l : 0.0f;
-  __bf16* dst = (__bf16*)(a.out + (long long)r * a.out_stride_b + (long long)hq * (D * 2));
 #pragma unroll
-  for (int i = 0; i < PER; ++i) dst[lane * PER + i] = (__bf16)(acc[i] * inv);
-  const float lse2 = len > 0 ? m + __log2f(l) : -INFINITY;
-  if (lane == 0 && a.lse != nullptr) a.lse[(long long)hq * a.lse_stride + r] = lse2 * 0.69314718055994530942f;
-  if (lane == 0 && a.lse2 != nullptr) a.lse2[(long long)r * a.Hq + hq] = lse2;
+  for (int i = 0; i < PER; ++i) sacc[wave][i * 64 + lane] = acc[i];
+  if (lane == 0) sl[wave] = l;
+  __syncthreads();
+  if (threadIdx.x >= D) return;
+  float sum = 0.0f;
+  l = 0.0f;
+  for (int w = 0; w < waves; ++w) {
+    l += sl[w];
+    sum += sacc[w][threadIdx.x];
+  }
+  __bf16* dst = (__bf16*)(a.out + (long long)r * a.out_stride_b + (long long)hq * (D * 2));
+  dst[threadIdx.x] = (__bf16)(empty ? 0.0f : sum * (1.0f / l));
+  const float lse2 = empty ? -INFINITY : m + __log2f(l);
+  if (threadIdx.x == 0 && a.lse != nullptr) a.lse[(long long)hq * a.lse_stride + r] = lse2 * 0.69314718055994530942f;
+  if (threadIdx.x == 0 && a.lse2 != nullptr) a.lse2[(long long)r * a.Hq + hq] = lse2;
 }
 
 // Accumulated weight: the query heads' weights of a token added in order, their mean onto what it had.
@@ -433,22 +619,27 @@ __global__ __launch_bounds__(256) void k_q4_mass(Q4AttnArgs a) {
   if (i >= len) return;
   const float* x = a.logits + (long long)r * a.Hq * a.logit_stride + i;
   float sum = 0.0f;
+#pragma unroll 8
   for (int h = 0; h < a.Hq; ++h) sum += exp2_of(x[h * a.logit_stride] - a.lse2[(long long)r * a.Hq + h]);
   const long long at = (long long)r * a.mass_stride + i;
   a.mass_out[at] = (a.mass_in != nullptr ? a.mass_in[at] : 0.0f) + sum / (float)a.Hq;
 }
 
+template <int D, bool MASS>
+hipError_t launch_q4_pass(const Q4AttnArgs& a, hipStream_t s) {
+  const dim3 grid(a.groups, 1, a.head_groups * ((a.Gq + 15) / 16)), block(64 * q4_waves(D));
+  hipLaunchKernelGGL((k_q4_attn<D, MASS>), grid, block, 0, s, a);
+  return hipGetLastError();
+}
+
 template <int D>
 hipError_t launch_q4_attn(const Q4AttnArgs& a, hipStream_t s) {
-  const dim3 grid(a.parts, a.R, a.head_groups * ((a.Gq + 15) / 16)), block(64 * q4_waves(D));
-  if (a.mass_out != nullptr) hipLaunchKernelGGL((k_q4_attn<D, true>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((k_q4_attn<D, false>), grid, block, 0, s, a);
-  hipError_t e = hipGetLastError();
+  hipError_t e = a.mass_out != nullptr ? launch_q4_pass<D, true>(a, s) : launch_q4_pass<D, false>(a, s);
   if (e != hipSuccess) return e;
-  if (a.parts * a.wave_parts > 1) {
-    hipLaunchKernelGGL((k_q4_join<D>), dim3((a.Hq + 3) / 4, a.R), dim3(256), 0, s, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
+  // (up to eight pieces per wave: one round of loads)
+  const int waves = a.groups * a.wave_parts > 32 * a.R ? kQ4JoinWaves : 4;
+  hipLaunchKernelGGL((k_q4_join<D>), dim3(a.Hq, a.R), dim3(64 * waves), 0, s, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
   if (a.mass_out != nullptr && a.max_len > 0) {
     hipLaunchKernelGGL(k_q4_mass, dim3((a.max_len + 255) / 256, a.R), dim3(256), 0, s, a);
     e = hipGetLastError();
