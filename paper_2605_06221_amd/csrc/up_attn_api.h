@@ -107,7 +107,7 @@ int q4_copy_impl(bool store, const up_params* p, const void* k, const void* v, i
   if ((k == nullptr) != (k_cache == nullptr) || (v == nullptr) != (v_cache == nullptr)) return UP_ERR_NULL;
   if ((k == nullptr && v == nullptr) || slots == nullptr) return UP_ERR_NULL;
   if (!aligned16(k) || !aligned16(v) || !aligned_to(slots, 8) || !aligned_to(count_dev, 4)) return UP_ERR_ALIGN;
-  if (n > INT32_MAX) return UP_ERR_UNSUPPORTED;
+  if (n > (INT32_MAX - 256) / ((int64_t)pb.Hkv * (pb.head_dim / kQ4Group))) return UP_ERR_UNSUPPORTED;      // groups of 64 elements
   Q4CopyArgs a{};
   a.rows_in[0] = (const char*)k; a.rows_in[1] = (const char*)v;
   a.rows_out[0] = (char*)const_cast<void*>(k); a.rows_out[1] = (char*)const_cast<void*>(v);

@@ -27,110 +27,145 @@ __device__ __forceinline__ unsigned pack2(float a, float b) {
   return __builtin_bit_cast(unsigned, __builtin_convertvector(v, bf16x2));
 }
 
+// (by value: a bit cast straight from an element of a vector takes the vector's first)
+__device__ __forceinline__ float word_float(unsigned w) { return __builtin_bit_cast(float, w); }
+
 // bits of the largest bf16 not above x, in the upper half of the word
 __device__ __forceinline__ unsigned bf16_below(float x) {
   const unsigned b = __builtin_bit_cast(unsigned, x);
   return (b >> 31 ? b + 0xffffu : b) & 0xffff0000u;
 }
-// bits of the smallest bf16 not below x >= 0
-__device__ __forceinline__ unsigned bf16_above(double x) {
-  unsigned b = __builtin_bit_cast(unsigned, (float)x) & 0xffff0000u;
-  if ((double)__builtin_bit_cast(float, b) < x) b += 0x10000u;
+// Bits of the smallest bf16 not below range / 15, range >= 0.  A bf16 times 15 is exact, so the comparison decides the quotient
+// without a division; the estimate it starts from is the one truncated to bf16 or the next.
+__device__ __forceinline__ unsigned step_of(double range) {
+  unsigned b = __builtin_bit_cast(unsigned, (float)(range * (1.0 / 15.0))) & 0xffff0000u;
+  if (b > 0 && 15.0 * (double)__builtin_bit_cast(float, b - 0x10000u) >= range) b -= 0x10000u;
+  else if (15.0 * (double)__builtin_bit_cast(float, b) < range) b += 0x10000u;
   return b;
 }
 
-// Eight lanes hold the 64 elements of a group, eight each.  A work-group takes kQ4Rows rows of keys and
-// of values; its units are (row, keys or values, group), eight lanes per unit, so that a wave
-// reads 1 KB of consecutive row bytes (bf16).
-constexpr int kQ4Rows = 2;
-struct Q4Unit { int t, kv, g; bool live; };
-__device__ __forceinline__ Q4Unit q4_unit(const Q4CopyArgs& a, int unit, int groups, unsigned magic) {
-  unsigned row, rest;
-  divmod_by((unsigned)unit, 2u * groups, magic, row, rest);
-  Q4Unit u;
-  u.kv = (int)rest >= groups;
-  u.g = (int)rest - u.kv * groups;
-  const long long t = (long long)blockIdx.x * kQ4Rows + row;
+// Eight lanes hold the 64 elements of a group, eight each.  The groups of all rows stand in a row; a work-group takes 4 x 32 of
+// them of the keys (blockIdx.y 0) or of the values, and every thread issues its four loads before it looks at one: bound by
+// memory, 16 bytes per lane and load on the wide side.
+constexpr int kQ4Units = 4;
+struct Q4Unit { bool live; int64_t slot; int t, g; };
+__device__ __forceinline__ void q4_units(const Q4CopyArgs& a, int groups, Q4Unit (&u)[kQ4Units]) {
+  const unsigned magic = 0xFFFFFFFFu / (unsigned)groups;
   const long long n = a.count_dev != nullptr && a.count_dev[0] < a.n ? a.count_dev[0] : a.n;
-  u.live = (int)row < kQ4Rows && t < n && a.cache[u.kv] != nullptr;
-  u.t = (int)t;
-  return u;
+#pragma unroll
+  for (int i = 0; i < kQ4Units; ++i) {
+    unsigned t, g;
+    divmod_by((blockIdx.x * kQ4Units + i) * 32u + (threadIdx.x >> 3), (unsigned)groups, magic, t, g);
+    u[i].t = (int)t;
+    u[i].g = (int)g;
+    u[i].live = (long long)t < n;
+    u[i].slot = u[i].live ? a.slots[t] : -1;
+  }
+#pragma unroll
+  for (int i = 0; i < kQ4Units; ++i) u[i].live = u[i].slot >= 0 && u[i].slot < a.num_slots;
 }
 
 template <bool F32>
 __global__ __launch_bounds__(256) void k_q4_store(Q4CopyArgs a) {
-  const int groups = a.heads * (a.D / kQ4Group), sub = threadIdx.x & 7;
-  const unsigned magic = 0xFFFFFFFFu / (2u * groups);
+  const int kv = blockIdx.y, sub = threadIdx.x & 7;
+  if (a.cache[kv] == nullptr) return;
+  const int groups = a.heads * (a.D / kQ4Group);
   const long long codes = q4_code_bytes(a.heads, a.D);
-  for (int unit = threadIdx.x >> 3; unit < kQ4Rows * 2 * groups; unit += 32) {
-    const Q4Unit u = q4_unit(a, unit, groups, magic);
-    if (!u.live) continue;
-    const int64_t slot = a.slots[u.t];
-    if (slot < 0 || slot >= a.num_slots) continue;
-    const char* src = a.rows_in[u.kv] + (long long)u.t * a.row_stride_b[u.kv] + (long long)(u.g * 8 + sub) * (F32 ? 32 : 16);
+  Q4Unit u[kQ4Units];
+  q4_units(a, groups, u);
+  constexpr int PER = F32 ? 2 : 1;
+  u32x4 w[kQ4Units][PER];
+#pragma unroll
+  for (int i = 0; i < kQ4Units; ++i) {
+    const char* src = a.rows_in[kv] + (long long)u[i].t * a.row_stride_b[kv] + (u[i].g * 8 + sub) * (F32 ? 32 : 16);
+#pragma unroll
+    for (int j = 0; j < PER; ++j) w[i][j] = u[i].live ? __builtin_nontemporal_load((const u32x4*)src + j) : u32x4{0, 0, 0, 0};
+  }
+#pragma unroll
+  for (int i = 0; i < kQ4Units; ++i) {
     float x[8];
-    if (F32) {
-      const f32x4 lo4 = ((const f32x4*)src)[0], hi4 = ((const f32x4*)src)[1];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) { x[i] = lo4[i]; x[4 + i] = hi4[i]; }
-    } else {
-      const u32x4 w = *(const u32x4*)src;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) { x[2 * i] = bf16_lo(w[i]); x[2 * i + 1] = bf16_hi(w[i]); }
+    for (int e = 0; e < 4; ++e) {
+      x[2 * e] = F32 ? word_float(w[i][F32 ? e / 2 : 0][(2 * e) & 3]) : bf16_lo(w[i][0][e]);
+      x[2 * e + 1] = F32 ? word_float(w[i][F32 ? e / 2 : 0][(2 * e + 1) & 3]) : bf16_hi(w[i][0][e]);
     }
-    float mn = x[0], mx = x[0];
-#pragma unroll
-    for (int i = 1; i < 8; ++i) { mn = fminf(mn, x[i]); mx = fmaxf(mx, x[i]); }
+    float mn = fminf(fminf(x[0], x[1]), x[2]), mx = fmaxf(fmaxf(x[0], x[1]), x[2]);
+    mn = fminf(fminf(mn, x[3]), x[4]); mx = fmaxf(fmaxf(mx, x[3]), x[4]);
+    mn = fminf(fminf(mn, x[5]), x[6]); mx = fmaxf(fmaxf(mx, x[5]), x[6]);
+    mn = fminf(mn, x[7]); mx = fmaxf(mx, x[7]);
     mn = fminf(mn, lane_dpp<0xB1>(mn)); mx = fmaxf(mx, lane_dpp<0xB1>(mx));
     mn = fminf(mn, lane_dpp<0x4E>(mn)); mx = fmaxf(mx, lane_dpp<0x4E>(mx));
     mn = fminf(mn, lane_dpp<0x141>(mn)); mx = fmaxf(mx, lane_dpp<0x141>(mx));
     const unsigned lo_bits = bf16_below(mn);
-    const float lo = __builtin_bit_cast(float, lo_bits);
-    const unsigned step_bits = bf16_above(((double)mx - (double)lo) / 15.0);
-    const float step = __builtin_bit_cast(float, step_bits);
-    // The quotient in float is off by less than 2^-20 here; a code is decided in double where that could
-    // matter (next to a half), and for steps whose reciprocal or range leaves the float range.
-    const bool wide = !(step > 1e-30f && step < 1e30f);
-    const float inv = 1.0f / step;
+    const float lo = word_float(lo_bits);
+    const unsigned step_bits = step_of((double)mx - (double)lo);
+    const float step = word_float(step_bits);
+    // The quotient in float may be off by 3e-6 (15 times three roundings), so a code is judged by what it leaves: the rest
+    // (x - lo) - code * step is exact in float whenever x - lo is.  Rests next to half a step -- one in 340 of normal bf16 elements is a
+    // true tie -- are looked at once more, in double where x - lo was rounded; so are steps whose reciprocal or range
+    // leaves the float range.
+    const float inv = __builtin_amdgcn_rcpf(step), half = 0.5f * step;
+    float code[8], rest[8], far = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float d = x[e] - lo;
+      code[e] = rintf(d * inv);
+      rest[e] = fmaf(-code[e], step, d);
+      far = fmaxf(far, fabsf(rest[e]));
+    }
+    const bool plain = step > 1e-30f && step < 1e30f;
+    if (!plain || far > half * 0.99999f) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float d = x[e] - lo, off = fabsf(rest[e]);
+        if (plain && off <= half * 0.99999f) continue;
+        if (plain && d + lo == x[e] && x[e] - d == lo) {
+          const bool odd = (unsigned)code[e] & 1u;
+          if (off > half || (off == half && odd)) code[e] += rest[e] > 0.0f ? 1.0f : -1.0f;
+        } else {
+          const double c = step > 0.0f ? rint(((double)x[e] - (double)lo) / (double)step) : 0.0;
+          code[e] = (float)fmin(fmax(c, 0.0), 15.0);
+        }
+      }
+    }
     unsigned packed = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float c = (x[i] - lo) * inv;
-      const float off = c - floorf(c) - 0.5f;
-      if (wide || fabsf(off) < 1e-3f) c = step > 0.0f ? (float)rint(((double)x[i] - (double)lo) / (double)step) : 0.0f;
-      else c = rintf(c);
-      const unsigned code = (unsigned)fminf(fmaxf(c, 0.0f), 15.0f);
-      packed |= code << (4 * i);
-    }
-    char* dst = a.cache[u.kv] + (long long)slot * a.cache_stride;
-    *(unsigned*)(dst + u.g * 32 + sub * 4) = packed;
-    if (sub == 0) *(unsigned*)(dst + codes + (long long)u.g * 4) = (lo_bits >> 16) | step_bits;
+    for (int e = 0; e < 8; ++e) packed |= ((unsigned)code[e] & 15u) << (4 * e);
+    if (!u[i].live) continue;
+    char* dst = a.cache[kv] + (long long)u[i].slot * a.cache_stride;
+    *(unsigned*)(dst + u[i].g * 32 + sub * 4) = packed;
+    if (sub == 0) *(unsigned*)(dst + codes + (long long)u[i].g * 4) = (lo_bits >> 16) | step_bits;
   }
 }
 
 template <bool F32>
 __global__ __launch_bounds__(256) void k_q4_load(Q4CopyArgs a) {
-  const int groups = a.heads * (a.D / kQ4Group), sub = threadIdx.x & 7;
-  const unsigned magic = 0xFFFFFFFFu / (2u * groups);
+  const int kv = blockIdx.y, sub = threadIdx.x & 7;
+  if (a.cache[kv] == nullptr) return;
+  const int groups = a.heads * (a.D / kQ4Group);
   const long long codes = q4_code_bytes(a.heads, a.D);
-  for (int unit = threadIdx.x >> 3; unit < kQ4Rows * 2 * groups; unit += 32) {
-    const Q4Unit u = q4_unit(a, unit, groups, magic);
-    if (!u.live) continue;
-    const int64_t slot = a.slots[u.t];
-    if (slot < 0 || slot >= a.num_slots) continue;
-    const char* src = a.cache[u.kv] + (long long)slot * a.cache_stride;
-    const unsigned packed = *(const unsigned*)(src + u.g * 32 + sub * 4);
-    const unsigned pair = *(const unsigned*)(src + codes + (long long)u.g * 4);
-    const float lo = bf16_lo(pair), step = bf16_hi(pair);
+  Q4Unit u[kQ4Units];
+  q4_units(a, groups, u);
+  unsigned packed[kQ4Units], pair[kQ4Units];
+#pragma unroll
+  for (int i = 0; i < kQ4Units; ++i) {
+    const char* src = a.cache[kv] + (u[i].live ? u[i].slot : 0) * a.cache_stride;
+    packed[i] = u[i].live ? *(const unsigned*)(src + u[i].g * 32 + sub * 4) : 0u;
+    pair[i] = u[i].live ? *(const unsigned*)(src + codes + (long long)u[i].g * 4) : 0u;
+  }
+#pragma unroll
+  for (int i = 0; i < kQ4Units; ++i) {
+    if (!u[i].live) continue;
+    const float lo = bf16_lo(pair[i]), step = bf16_hi(pair[i]);
     float x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = fmaf((float)((packed >> (4 * i)) & 15u), step, lo);
-    char* dst = a.rows_out[u.kv] + (long long)u.t * a.row_stride_b[u.kv] + (long long)(u.g * 8 + sub) * (F32 ? 32 : 16);
+    for (int e = 0; e < 8; ++e) x[e] = fmaf((float)((packed[i] >> (4 * e)) & 15u), step, lo);
+    char* dst = a.rows_out[kv] + (long long)u[i].t * a.row_stride_b[kv] + (u[i].g * 8 + sub) * (F32 ? 32 : 16);
     if (F32) {
-      ((f32x4*)dst)[0] = f32x4{x[0], x[1], x[2], x[3]};
-      ((f32x4*)dst)[1] = f32x4{x[4], x[5], x[6], x[7]};
+      __builtin_nontemporal_store(f32x4{x[0], x[1], x[2], x[3]}, (f32x4*)dst);
+      __builtin_nontemporal_store(f32x4{x[4], x[5], x[6], x[7]}, (f32x4*)dst + 1);
     } else {
-      *(u32x4*)dst = u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])};
+      __builtin_nontemporal_store(u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])}, (u32x4*)dst);
     }
   }
 }
@@ -647,17 +682,22 @@ hipError_t launch_q4_attn(const Q4AttnArgs& a, hipStream_t s) {
   return e;
 }
 
+dim3 q4_copy_grid(const Q4CopyArgs& a) {
+  const long long units = a.n * a.heads * (a.D / kQ4Group), each = 32 * kQ4Units;
+  return dim3((unsigned)((units + each - 1) / each), 2);
+}
+
 }  // namespace
 
 hipError_t launch_q4_store(const Q4CopyArgs& a, bool f32, hipStream_t s) {
-  const dim3 grid((unsigned)((a.n + kQ4Rows - 1) / kQ4Rows));
+  const dim3 grid = q4_copy_grid(a);
   if (f32) hipLaunchKernelGGL((k_q4_store<true>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((k_q4_store<false>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
 hipError_t launch_q4_load(const Q4CopyArgs& a, bool f32, hipStream_t s) {
-  const dim3 grid((unsigned)((a.n + kQ4Rows - 1) / kQ4Rows));
+  const dim3 grid = q4_copy_grid(a);
   if (f32) hipLaunchKernelGGL((k_q4_load<true>), grid, dim3(256), 0, s, a);
   else hipLaunchKernelGGL((k_q4_load<false>), grid, dim3(256), 0, s, a);
   return hipGetLastError();
