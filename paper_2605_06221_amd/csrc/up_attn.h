@@ -98,7 +98,7 @@ struct EvictArgs {
   int32_t* kept_idx;                // [R][mass_out_stride]
   int32_t* new_len;
   int R, max_len, budget, n_sink, n_recent, kv_block;
-  unsigned kv_magic;
+  unsigned kv_magic, piece_magic;   // 0xFFFFFFFF / kv_block, 0xFFFFFFFF / (row_bytes / 16)
 };
 
 #if defined(__HIPCC__)
