@@ -23,10 +23,15 @@ struct AttnGeometry {
   size_t base_off, o_off, ml_off, total;
 };
 
-constexpr long long kAttnMinPart = 1024;
+// What a cut gains and costs, in microseconds.  A CU works through the keys of 128 rows at key_us each; with the keys cut into
+// pieces of half a CU's share, not the longest tile decides but the share and one piece more.  Every piece then leaves float rows that are written and read back (3 TB/s) by one more launch.
+// key_us is measured (one tile on a CU of its own); batches on both sides of the rule, not cut -> cut: one token after 8191, 56 -> 28 us
+// (in pieces of 2048 and of 512 keys); 1000 tokens float, 8/8 heads, 137 -> 57; 2048 tokens, 32/8 heads, 67 -> 98 (not cut);
+// 1000 tokens, 32/8 heads, 28 -> 39 (not cut).  Pieces shorter than 512 keys (256 float) cost more to join than they save.
+double attn_key_us(bool f32, int D) { return f32 ? (D == 64 ? 0.06 : 0.13) : D == 64 ? 0.01 : D == 128 ? 0.015 : 0.04; }
 
 int attn_geometry(const Problem& pb, const int32_t* cu, const int32_t* ck, AttnGeometry* g) {
-  const int D = pb.head_dim, row_bytes = D * (pb.qk_is_f32 ? 4 : 2);
+  const int D = pb.head_dim;
   *g = AttnGeometry{};
   g->rows = 256;
   long long longest = 0, live = 0;
@@ -45,13 +50,18 @@ int attn_geometry(const Problem& pb, const int32_t* cu, const int32_t* ck, AttnG
   g->parts = 1;
   g->slots = (long long)pb.T * pb.Gq / g->rows + pb.R;
   g->items = g->slots;
-  // work-groups that the chip holds at once
-  const int places = kCUs * (row_bytes == 512 ? 1 : row_bytes == 128 ? 1024 / g->rows / 2 : 256 / g->rows);
-  const double fair = work * pb.Hkv / places;      // keys per place if all finished together
-  if ((double)longest > fair && longest > kAttnMinPart) {
-    const long long want = fair > (double)kAttnMinPart ? (long long)fair : kAttnMinPart;
+  const double fair = work * pb.Hkv / kCUs;      // keys per CU
+  const long long fewest = pb.qk_is_f32 ? 256 : 512;
+  if ((double)longest > fair && longest > fewest) {
+    const long long want = fair > 2.0 * (double)fewest ? (long long)(0.5 * fair) : fewest;
     const long long part = (want + 127) / 128 * 128;
-    if (part < longest) {
+    double rows = 0;      // rows of float sums that the pieces leave
+    for (int r = 0; r < pb.R; ++r) {
+      const long long N = cu[r + 1] - cu[r], n = (ck[r + 1] - ck[r] + part - 1) / part;
+      if (n > 1) rows += (double)(N * pb.Hq) * (double)n;
+    }
+    const double gain = ((double)longest - fair - (double)part) * attn_key_us(pb.qk_is_f32, D) * g->rows / 128, cost = 6.0 + rows * D * 8.0 / 3e6;
+    if (part < longest && gain > cost) {
       g->part_keys = (int)part;
       g->parts = (int)((longest + part - 1) / part);
       g->items = 0;
