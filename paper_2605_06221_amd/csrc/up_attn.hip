@@ -269,7 +269,12 @@ __global__ __launch_bounds__(64 * WAVES, (AttnTile<F32, D, WAVES>::DENSE)) void 
   float m = -INFINITY, l = 0.0f;
 
   // MASK: some keys of the tile come after some rows of the wave
+  // The permuted place of piece p is that of piece 0 with p's bits turned over, so a lane's addresses are one constant and an exclusive or
+  // each.  For 512-byte rows the constant is made anew in every tile: kept over the loop, the addresses pushed accumulators into
+  // scratch (72 registers of it, 4.84 ms for a prompt of 16384 with 16 heads; now 25 and 1.98 ms).
   auto tile = [&](auto mask_tag, int k0, const u32x4* sk, const u32x4* sv) __attribute__((always_inline)) {
+    unsigned k_from = (unsigned)k_place<T::PPR>(l32, F32 ? half * (T::PPR / 2) : half) * 16u;
+    if constexpr (T::SRCB == 512) asm volatile("" : "+v"(k_from));
     f32x16 s[T::SUB];
 #pragma unroll
     for (int sub = 0; sub < T::SUB; ++sub) {
@@ -277,7 +282,7 @@ __global__ __launch_bounds__(64 * WAVES, (AttnTile<F32, D, WAVES>::DENSE)) void 
       for (int e = 0; e < 16; ++e) s[sub][e] = 0.0f;
 #pragma unroll
       for (int kk = 0; kk < T::KREG; ++kk) {
-        const u32x4 k4 = sk[k_place<T::PPR>(sub * 32 + l32, F32 ? half * (T::PPR / 2) + kk : 2 * kk + half)];
+        const u32x4 k4 = *(const u32x4*)((const char*)sk + (k_from ^ (unsigned)(kk * KSTEP)) + sub * 32 * T::SRCB);
         if (F32) {
           const u32x4 q4 = qf[kk];
 #pragma unroll
@@ -346,6 +351,14 @@ __global__ __launch_bounds__(64 * WAVES, (AttnTile<F32, D, WAVES>::DENSE)) void 
       // read gives 16 lanes a column each of 4 rows x 16 columns: its lane i points at row i/4, columns 4*(i%4)..
       const int vrow = 4 * half + ((lane >> 2) & 3);
       const int vpc = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), vlo = (lane & 1) * 8;
+      unsigned v_from = (unsigned)v_place<T::PPR, F32>(vrow, vpc) * 16u + vlo;
+      if constexpr (T::SRCB == 512) asm volatile("" : "+v"(v_from));
+      // columns 32*dt.. of keys `row`.. of the tile.  (Rows of 256 bytes and fewer are indexed plainly: with the exclusive or, the
+      // 128-wide kernel came out 1.2 % slower, 7.88 against 7.79 ms for a prompt of 32768.)
+      auto v_at = [&](int row, int dt) __attribute__((always_inline)) {
+        if constexpr (T::SRCB == 512) return (const char*)sv + (v_from ^ (unsigned)(dt * 64)) + row * T::SRCB;
+        else return (const char*)&sv[v_place<T::PPR, F32>(row + vrow, dt * 4 + vpc)] + vlo;
+      };
 #pragma unroll
       for (int sub = 0; sub < T::SUB; ++sub)
 #pragma unroll
@@ -357,10 +370,10 @@ __global__ __launch_bounds__(64 * WAVES, (AttnTile<F32, D, WAVES>::DENSE)) void 
           pw.w = pack_bf16(s[sub][8 * st + 6], s[sub][8 * st + 7]);
 #pragma unroll
           for (int dt = 0; dt < T::DT; ++dt) {
-            const int r0 = sub * 32 + st * 16 + vrow;
+            const int row = sub * 32 + st * 16;
             typedef __attribute__((address_space(3))) s16x4* lds4;
-            const s16x4 va = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)((__attribute__((address_space(3))) char*)&sv[v_place<T::PPR, F32>(r0, dt * 4 + vpc)] + vlo));
-            const s16x4 vb = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)((__attribute__((address_space(3))) char*)&sv[v_place<T::PPR, F32>(r0 + 8, dt * 4 + vpc)] + vlo));
+            const s16x4 va = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(__attribute__((address_space(3))) char*)v_at(row, dt));
+            const s16x4 vb = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(__attribute__((address_space(3))) char*)v_at(row + 8, dt));
             u32x4 vv;
             vv.x = __builtin_bit_cast(u32x2, va).x;
             vv.y = __builtin_bit_cast(u32x2, va).y;
