@@ -583,10 +583,12 @@ int uniprefill_attention_q4(const up_params* p, const void* q, const void* k_cac
  *   prefix) stay intact, and freeing the old pages is the caller's.
  *   kept_idx [num_seqs][mass_out_stride] and mass_out [num_seqs][mass_out_stride]
  *   (mass_out_stride >= budget, UP_ERR_SHAPE): entries j < new_len[r] are written;
- *   kept_idx is ascending.  mass must be finite.  Both block tables have rows of
+ *   kept_idx is ascending.  mass must be finite.  kept_idx and mass_out overlap neither each other nor
+ *   mass: a row of mass_out also holds the counts of a long sequence's choice while the call runs.  Both block tables have rows of
  *   kv_block_size-token pages that hold max_kv_len (block_table) and the smaller of
  *   budget and max_kv_len (new_table) tokens, else UP_ERR_SHAPE.  row_bytes, cache_row_stride:
- *   multiples of 16 (UP_ERR_ALIGN), row_bytes >= 16 and <= cache_row_stride. */
+ *   multiples of 16 (UP_ERR_ALIGN), row_bytes >= 16 and <= cache_row_stride.  More than 65535
+ *   sequences, max_kv_len above 2^31 - 65537, or a row of 2^31 kept 16-byte pieces and more: UP_ERR_UNSUPPORTED. */
 int uniprefill_cache_evict(void* k_cache, void* v_cache, int64_t row_bytes, int64_t cache_row_stride,
                            const float* mass, int64_t mass_row_stride, const int32_t* kv_len_dev,
                            int32_t num_seqs, int32_t max_kv_len, int32_t budget, int32_t n_sink,

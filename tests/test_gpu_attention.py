@@ -471,6 +471,10 @@ def _mass(rng, kind, n):
     ([1], 1, 0, 0, 16, 16), ([5, 0, 64, 65, 1000], 64, 4, 4, 16, 144), ([3000, 10, 2049], 300, 128, 128, 7, 576),
     ([100], 100, 50, 50, 16, 32), ([101, 500], 100, 50, 50, 1, 1040), ([20000, 16385], 5000, 0, 1, 32, 64), ([700], 699, 3, 0, 16, 32),
     ([64], 1, 1, 0, 16, 16),
+    # long ones: many work-groups to a sequence, without a choice to make, with one token too little room for it; one work-group and masses
+    # of one first digit beyond what its LDS holds
+    ([60000, 24577, 0, 9, 8999, 30000], 9000, 4, 100, 64, 16), ([40000, 12000], 12000, 6000, 6000, 128, 16), ([24576], 6164, 0, 0, 16, 16),
+    ([24576], 6163, 0, 0, 16, 16), ([70000, 30000], 300, 16, 16, 64, 16), ([70000, 26000], 25500, 0, 0, 64, 16),
 ])
 def test_eviction(lengths, budget, n_sink, n_recent, page, row_bytes, kind):
     _say("eviction", lengths, budget, n_sink, n_recent, page, row_bytes, kind)
