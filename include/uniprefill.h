@@ -480,7 +480,12 @@ int uniprefill_fused_top_p_chunked(const up_params* p, const void* q, const void
  * k_row_stride, softmax_scale and qk_dtype (the drop layer's parameters may be
  * handed over as they are).  Query, key and value rows must be finite where a
  * token reads them; what lies beyond the sequences is never read into a result.
- * Batches of more than 2^31 - 1 work items are refused (UP_ERR_UNSUPPORTED). */
+ * UP_ERR_UNSUPPORTED: batches of more than 2^31 - 1 work items, sequences (max_kv_len) of more than
+ * 2^31 - 65537 tokens, key or value rows more than 2^27 bytes apart in uniprefill_attention, more
+ * than 65535 sequences over the 4-bit cache.
+ * None of these calls waits for the device or allocates; all can be captured into a graph (the host
+ * arrays are read when the call is made).  A workspace is free again when the call's work has run: calls that may run at the same
+ * time need one each. */
 
 /* Causal attention of a packed batch (Eq. 2; "Sparsity Propagation": the layer
  * whose queries and keys are scored): token i of sequence r, with P_r earlier
@@ -495,7 +500,8 @@ int uniprefill_fused_top_p_chunked(const up_params* p, const void* q, const void
  * batch of its own (new_cu_seqlens): the order of its tokens is what is causal.
  *   v                 like k, v_row_stride elements between tokens
  *   out               [T, num_q_heads, head_dim] in qk_dtype, out_row_stride
- *                     elements between tokens; only the batch's rows are written
+ *                     elements between tokens; only the batch's rows are written;
+ *                     overlaps none of q, k, v
  *   lse_out           float, may be NULL; lse_row_stride >= total_tokens (UP_ERR_SHAPE)
  *   workspace         from uniprefill_attention_plan (256-byte aligned): room to
  *                     split long key ranges of few query rows; 0 bytes (and NULL)
@@ -522,6 +528,7 @@ int uniprefill_attention(const up_params* p, const void* q, const void* k, const
  *     step   = the smallest bf16 not below (maximum - lowest) / 15,
  *     code   = (element - lowest) / step rounded to the nearest whole number,
  *              ties to even, at most 15 (0 where step is 0).
+ * (UP_F32 elements must lie within the range of bf16.)
  * uniprefill_q4_row_bytes: bytes of a row; 0 for a head_dim other than 64, 128,
  * 256 or num_kv_heads < 1.
  *

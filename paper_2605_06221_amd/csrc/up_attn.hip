@@ -8,14 +8,19 @@
 //
 // Work decomposition: a work-group is 8 (or 4) waves x 32 rows.  A row is a (token, query head) pair of one kv
 // head, token-major, so the query heads that share keys share a tile and a single token is a small
-// batch too.  Keys and values pass through LDS in tiles of 64 (32 where a head row has 512 bytes), double-buffered,
-// fetched into registers while the tile before them is worked on.
+// batch too.  Keys and values pass through LDS in tiles of 64 (32 where a head row has 512 bytes), two tiles at a time with eight waves,
+// double-buffered, and loaded into it directly while the ones before them are worked on.  (Fetched into registers and written to LDS from there, with
+// 128 rows per work-group: 9.31 ms for a prompt of 32768, 32/8 heads of 128; so 7.77 ms, 1.13 PFLOP/s.)
 //
 // The products are formed transposed: S^T = K Q^T leaves a lane with one query row and half of the
 // tile's keys, so the softmax statistics are sums inside a lane and one exchange between lane
 // halves, and the weights already sit in the operand layout of O^T = V^T P^T: the contraction runs over
 // the keys in the order in which the lanes hold them.  V^T comes out of row-major LDS through the
 // transposing read (bf16) or plain reads (float operands).
+//
+// Bound by the matrix cores and the exponentials beside them at the clock that the power leaves (a prompt of 32768: the matrix
+// cores busy in 59 % of the cycles at 1.7 GHz; a library's product of 8192^3 reaches 1.38 PFLOP/s); decode rows and short
+// chunks on long caches by the latency of a work-group's tiles, which is why their keys are cut.
 #include <type_traits>
 
 #include "up_attn.h"
@@ -268,10 +273,10 @@ __global__ __launch_bounds__(64 * WAVES, (AttnTile<F32, D, WAVES>::DENSE)) void 
     for (int e = 0; e < 16; ++e) o[dt][e] = 0.0f;
   float m = -INFINITY, l = 0.0f;
 
-  // MASK: some keys of the tile come after some rows of the wave
   // The permuted place of piece p is that of piece 0 with p's bits turned over, so a lane's addresses are one constant and an exclusive or
   // each.  For 512-byte rows the constant is made anew in every tile: kept over the loop, the addresses pushed accumulators into
   // scratch (72 registers of it, 4.84 ms for a prompt of 16384 with 16 heads; now 25 and 1.98 ms).
+  // mask_tag: some keys of the tile come after some rows of the wave.
   auto tile = [&](auto mask_tag, int k0, const u32x4* sk, const u32x4* sv) __attribute__((always_inline)) {
     unsigned k_from = (unsigned)k_place<T::PPR>(l32, F32 ? half * (T::PPR / 2) : half) * 16u;
     if constexpr (T::SRCB == 512) asm volatile("" : "+v"(k_from));

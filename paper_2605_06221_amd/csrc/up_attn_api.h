@@ -7,6 +7,11 @@
 
 namespace {
 
+// bytes between key (value) rows up to which a work-group's offsets of a few rows stay within 32 bits
+constexpr int64_t kMaxRowStride = 1 << 27;
+// tokens of a sequence up to which the kernels may count some tiles past its end
+constexpr int kMaxLength = INT32_MAX - 65536;
+
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // ---- attention of a packed batch
@@ -24,7 +29,8 @@ struct AttnGeometry {
 };
 
 // What a cut gains and costs, in microseconds.  A CU works through the keys of 128 rows at key_us each; with the keys cut into
-// pieces of half a CU's share, not the longest tile decides but the share and one piece more.  Every piece then leaves float rows that are written and read back (3 TB/s) by one more launch.
+// pieces of half a CU's share, not the longest tile decides but the share and one piece more.  Every piece then leaves float rows that are
+// written and read back (3 TB/s) by one more launch.
 // key_us is measured (one tile on a CU of its own); batches on both sides of the rule, not cut -> cut: one token after 8191, 56 -> 28 us
 // (in pieces of 2048 and of 512 keys); 1000 tokens float, 8/8 heads, 137 -> 57; 2048 tokens, 32/8 heads, 67 -> 98 (not cut);
 // 1000 tokens, 32/8 heads, 28 -> 39 (not cut).  Pieces shorter than 512 keys (256 float) cost more to join than they save.
@@ -40,6 +46,7 @@ int attn_geometry(const Problem& pb, const int32_t* cu, const int32_t* ck, AttnG
     live += (N * pb.Gq + 255) / 256;
     if (N > 0) longest = L > longest ? L : longest;
   }
+  if (longest > kMaxLength) return UP_ERR_UNSUPPORTED;
   if (live * pb.Hkv < kCUs) g->rows = 128;
   auto tiles_of = [&](long long N) { return (N * pb.Gq + g->rows - 1) / g->rows; };
   double work = 0;
@@ -90,9 +97,6 @@ int check_row_stride(int64_t stride, int heads, int head_dim, int elem) {
   if ((stride * elem) % 16 != 0) return UP_ERR_ALIGN;
   return UP_OK;
 }
-
-// bytes between key (value) rows up to which a work-group's offsets of a few rows stay within 32 bits
-constexpr int64_t kMaxRowStride = 1 << 27;
 
 bool aligned_to(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1u)) == 0; }
 
@@ -171,7 +175,7 @@ int q4_geometry(const Problem& pb, int max_len, bool mass, Q4Geometry* g) {
     off = align256(off + rows * (size_t)g->logit_stride * sizeof(float));
   }
   g->total = off;
-  if (pb.R > 65535 || layers > 65535 || steps > INT32_MAX) return UP_ERR_UNSUPPORTED;
+  if (pb.R > 65535 || layers > 65535 || steps > INT32_MAX || max_len > kMaxLength) return UP_ERR_UNSUPPORTED;
   return UP_OK;
 }
 
@@ -295,7 +299,6 @@ int uniprefill_attention_q4(const up_params* p, const void* q, const void* k_cac
   if (pb.R > 0 && (!q || !out || !kv_len_dev || (max_kv_len > 0 && (!k_cache || !v_cache)))) return UP_ERR_NULL;
   if (mass_in != nullptr && mass_out == nullptr) return UP_ERR_NULL;
   if ((st = check_q4_cache(pb, k_cache, v_cache, cache_row_stride)) != UP_OK) return st;
-  if (cache_row_stride > kMaxRowStride) return UP_ERR_UNSUPPORTED;
   if ((st = check_row_stride(out_row_stride, pb.Hq, pb.head_dim, 2)) != UP_OK) return st;
   if (pb.R > 0 && (st = check_table(block_table, block_table_stride, kv_block_size, max_kv_len)) != UP_OK) return st;
   if (lse_out != nullptr && lse_row_stride < pb.R) return UP_ERR_SHAPE;
@@ -348,7 +351,7 @@ int uniprefill_cache_evict(void* k_cache, void* v_cache, int64_t row_bytes, int6
   if ((st = check_table(new_table, new_table_stride, kv_block_size, most)) != UP_OK) return st;
   if (!aligned_to(mass, 4) || !aligned_to(mass_out, 4) || !aligned_to(kept_idx, 4) || !aligned_to(kv_len_dev, 4) || !aligned_to(new_len, 4))
     return UP_ERR_ALIGN;
-  if (num_seqs > 65535 || max_kv_len > INT32_MAX - 65536 || most > (INT32_MAX - 1024) / (row_bytes / 16)) return UP_ERR_UNSUPPORTED;
+  if (num_seqs > 65535 || max_kv_len > kMaxLength || most > (INT32_MAX - 1024) / (row_bytes / 16)) return UP_ERR_UNSUPPORTED;
   EvictArgs a{};
   a.k = (char*)k_cache; a.v = (char*)v_cache; a.row_bytes = row_bytes; a.cache_stride = cache_row_stride;
   a.mass = mass; a.mass_out = mass_out; a.mass_stride = mass_row_stride; a.mass_out_stride = mass_out_stride;

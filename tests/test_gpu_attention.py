@@ -418,6 +418,17 @@ def test_decode_over_the_cache(lengths, hq, hkv, D, page, mass):
     d.check()
 
 
+@pytest.mark.parametrize("R,hq,hkv,D", [(1100, 4, 2, 64), (513, 8, 8, 128), (600, 8, 4, 256)])
+def test_decode_of_more_sequences_than_a_work_group_has_threads(R, hq, hkv, D):
+    _say("decode: many sequences", R, hq, hkv, D)
+    rng = np.random.default_rng(R)
+    lengths = [int(n) for n in np.where(rng.random(R) < 0.2, 0, rng.integers(1, 200, R))]
+    lengths[-1] = 77
+    d = Decode(R, lengths, hq, hkv, D, mass=True)
+    d.run()
+    d.check()
+
+
 def test_decode_lengths_beyond_the_ends_count_as_the_ends():
     _say("decode: lengths out of range, room for longer caches than there are")
     d = Decode(4, [200, 0, 200], 8, 2, 128, mass=True, max_len=200)

@@ -180,3 +180,18 @@ def _evict(**kw):
 ])
 def test_evict_refusals(kw, want):
     assert _evict(**kw) == want
+
+
+def test_refusals_of_what_the_kernels_cannot_count():
+    wide = _params(k_row_stride=(1 << 26) + 8)      # bf16: more than 2^27 bytes
+    assert _attention(wide) == up.UP_ERR_UNSUPPORTED
+    assert _attention(v_stride=(1 << 26) + 8) == up.UP_ERR_UNSUPPORTED
+    most = (1 << 31) - 1 - 65536
+    for n, want in ((most, up.UP_OK), (most + 1, up.UP_ERR_UNSUPPORTED)):
+        cu, ck = np.array([0, 1], np.int32), np.array([0, n], np.int32)
+        assert up.uniprefill_attention_plan(_params(num_seqs=1, total_tokens=1), cu, ck, check=False)[0] == want
+        assert up.uniprefill_attention_q4_plan(_params(num_seqs=1, total_tokens=1), n, False, check=False)[0] == want
+    assert _evict(max_len=most + 1, mass_stride=1 << 32, tstride=1 << 32) == up.UP_ERR_UNSUPPORTED
+    # more 16-byte pieces of kept rows than are counted in 31 bits
+    assert _evict(max_len=1 << 30, mass_stride=1 << 30, tstride=1 << 30, budget=1 << 30, out_stride=1 << 30, nstride=1 << 30, row=64,
+                  stride=64) == up.UP_ERR_UNSUPPORTED
