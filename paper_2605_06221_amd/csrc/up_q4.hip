@@ -35,109 +35,141 @@ __device__ __forceinline__ unsigned bf16_below(float x) {
   const unsigned b = __builtin_bit_cast(unsigned, x);
   return (b >> 31 ? b + 0xffffu : b) & 0xffff0000u;
 }
-// Bits of the smallest bf16 not below range / 15, range >= 0.  A bf16 times 15 is exact, so the comparison decides the quotient
-// without a division; the estimate it starts from is the one truncated to bf16 or the next.
-__device__ __forceinline__ unsigned step_of(double range) {
+// Bits of the smallest bf16 not below (mx - lo) / 15.  A bf16 times 15 is exact, so the comparison decides the quotient without a
+// division.  In float, with the range as a sum of two floats, its estimate taken a little too large so that truncated to bf16 it is the
+// answer or the bf16 below; in double for ranges near the ends of the float range (and 0).
+__device__ __forceinline__ unsigned step_of(float mx, float lo) {
+  const float r = mx - lo;
+  if (r > 1e-30f && r < 1e30f) {
+    const float back = r - mx, rest = (mx - (r - back)) - (lo + back);      // r + rest = mx - lo
+    const unsigned b = __builtin_bit_cast(unsigned, r * (1.000001f / 15.0f)) & 0xffff0000u;
+    const float p = 15.0f * word_float(b);
+    return p > r || (p == r && rest <= 0.0f) ? b : b + 0x10000u;
+  }
+  const double range = (double)mx - (double)lo;
   unsigned b = __builtin_bit_cast(unsigned, (float)(range * (1.0 / 15.0))) & 0xffff0000u;
-  if (b > 0 && 15.0 * (double)__builtin_bit_cast(float, b - 0x10000u) >= range) b -= 0x10000u;
-  else if (15.0 * (double)__builtin_bit_cast(float, b) < range) b += 0x10000u;
+  if (b > 0 && 15.0 * (double)word_float(b - 0x10000u) >= range) b -= 0x10000u;
+  else if (15.0 * (double)word_float(b) < range) b += 0x10000u;
   return b;
 }
 
-// Eight lanes hold the 64 elements of a group, eight each.  The groups of all rows stand in a row; a work-group takes 4 x 32 of
-// them of the keys (blockIdx.y 0) or of the values, and every thread issues its four loads before it looks at one: bound by
-// memory, 16 bytes per lane and load on the wide side.
-constexpr int kQ4Units = 4;
+// LANES lanes hold the 64 elements of a group.  The groups of all rows stand in a row; a work-group takes UNITS x 256 / LANES of
+// them of the keys (blockIdx.y 0) or of the values, and every thread issues the loads of its UNITS before it looks at one.
+constexpr int kQ4Block = 128;      // groups per work-group
 struct Q4Unit { bool live; int64_t slot; int t, g; };
-__device__ __forceinline__ void q4_units(const Q4CopyArgs& a, int groups, Q4Unit (&u)[kQ4Units]) {
+template <int LANES, int UNITS>
+__device__ __forceinline__ void q4_units(const Q4CopyArgs& a, int groups, Q4Unit (&u)[UNITS]) {
+  static_assert(UNITS * 256 / LANES == kQ4Block, "the launch's grid");
   const unsigned magic = 0xFFFFFFFFu / (unsigned)groups;
   const long long n = a.count_dev != nullptr && a.count_dev[0] < a.n ? a.count_dev[0] : a.n;
 #pragma unroll
-  for (int i = 0; i < kQ4Units; ++i) {
+  for (int i = 0; i < UNITS; ++i) {
     unsigned t, g;
-    divmod_by((blockIdx.x * kQ4Units + i) * 32u + (threadIdx.x >> 3), (unsigned)groups, magic, t, g);
+    divmod_by((blockIdx.x * UNITS + i) * (256u / LANES) + threadIdx.x / LANES, (unsigned)groups, magic, t, g);
     u[i].t = (int)t;
     u[i].g = (int)g;
     u[i].live = (long long)t < n;
     u[i].slot = u[i].live ? a.slots[t] : -1;
   }
 #pragma unroll
-  for (int i = 0; i < kQ4Units; ++i) u[i].live = u[i].slot >= 0 && u[i].slot < a.num_slots;
+  for (int i = 0; i < UNITS; ++i) u[i].live = u[i].slot >= 0 && u[i].slot < a.num_slots;
 }
 
+// A lane takes two pieces of eight elements, so that what is done once per group (its place, the reduction over the lanes, the step) is
+// shared by sixteen.  (One piece per lane, eight lanes to a group, the step in double, and a branch for everything next to a tie, which some lane of
+// nearly every wave takes: bound by its instructions, 179 us for the keys and values of 131072 tokens, 8 heads of 128; so 143 us,
+// 4.8 TB/s, what a copy reaches.)
 template <bool F32>
 __global__ __launch_bounds__(256) void k_q4_store(Q4CopyArgs a) {
-  const int kv = blockIdx.y, sub = threadIdx.x & 7;
+  constexpr int LANES = 4, UNITS = 2, PIECES = 2, PER = F32 ? 2 : 1;
+  const int kv = blockIdx.y, sub = threadIdx.x & (LANES - 1);
   if (a.cache[kv] == nullptr) return;
   const int groups = a.heads * (a.D / kQ4Group);
   const long long codes = q4_code_bytes(a.heads, a.D);
-  Q4Unit u[kQ4Units];
-  q4_units(a, groups, u);
-  constexpr int PER = F32 ? 2 : 1;
-  u32x4 w[kQ4Units][PER];
+  Q4Unit u[UNITS];
+  q4_units<LANES, UNITS>(a, groups, u);
+  u32x4 w[UNITS][PIECES][PER];
 #pragma unroll
-  for (int i = 0; i < kQ4Units; ++i) {
+  for (int i = 0; i < UNITS; ++i) {
     const char* src = a.rows_in[kv] + (long long)u[i].t * a.row_stride_b[kv] + (u[i].g * 8 + sub) * (F32 ? 32 : 16);
 #pragma unroll
-    for (int j = 0; j < PER; ++j) w[i][j] = u[i].live ? __builtin_nontemporal_load((const u32x4*)src + j) : u32x4{0, 0, 0, 0};
+    for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+      for (int j = 0; j < PER; ++j)
+        w[i][p][j] = u[i].live ? __builtin_nontemporal_load((const u32x4*)src + p * LANES * PER + j) : u32x4{0, 0, 0, 0};
   }
 #pragma unroll
-  for (int i = 0; i < kQ4Units; ++i) {
-    float x[8];
+  for (int i = 0; i < UNITS; ++i) {
+    float x[PIECES][8], mn = INFINITY, mx = -INFINITY, least = INFINITY;      // least: the smallest magnitude
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      x[2 * e] = F32 ? word_float(w[i][F32 ? e / 2 : 0][(2 * e) & 3]) : bf16_lo(w[i][0][e]);
-      x[2 * e + 1] = F32 ? word_float(w[i][F32 ? e / 2 : 0][(2 * e + 1) & 3]) : bf16_hi(w[i][0][e]);
-    }
-    float mn = fminf(fminf(x[0], x[1]), x[2]), mx = fmaxf(fmaxf(x[0], x[1]), x[2]);
-    mn = fminf(fminf(mn, x[3]), x[4]); mx = fmaxf(fmaxf(mx, x[3]), x[4]);
-    mn = fminf(fminf(mn, x[5]), x[6]); mx = fmaxf(fmaxf(mx, x[5]), x[6]);
-    mn = fminf(mn, x[7]); mx = fmaxf(mx, x[7]);
-    mn = fminf(mn, lane_dpp<0xB1>(mn)); mx = fmaxf(mx, lane_dpp<0xB1>(mx));
-    mn = fminf(mn, lane_dpp<0x4E>(mn)); mx = fmaxf(mx, lane_dpp<0x4E>(mx));
-    mn = fminf(mn, lane_dpp<0x141>(mn)); mx = fmaxf(mx, lane_dpp<0x141>(mx));
-    const unsigned lo_bits = bf16_below(mn);
-    const float lo = word_float(lo_bits);
-    const unsigned step_bits = step_of((double)mx - (double)lo);
-    const float step = word_float(step_bits);
-    // The quotient in float may be off by 3e-6 (15 times three roundings), so a code is judged by what it leaves: the rest
-    // (x - lo) - code * step is exact in float whenever x - lo is.  Rests next to half a step -- one in 340 of normal bf16 elements is a
-    // true tie -- are looked at once more, in double where x - lo was rounded; so are steps whose reciprocal or range
-    // leaves the float range.
-    const float inv = __builtin_amdgcn_rcpf(step), half = 0.5f * step;
-    float code[8], rest[8], far = 0.0f;
+    for (int p = 0; p < PIECES; ++p) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float d = x[e] - lo;
-      code[e] = rintf(d * inv);
-      rest[e] = fmaf(-code[e], step, d);
-      far = fmaxf(far, fabsf(rest[e]));
-    }
-    const bool plain = step > 1e-30f && step < 1e30f;
-    if (!plain || far > half * 0.99999f) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const float d = x[e] - lo, off = fabsf(rest[e]);
-        if (plain && off <= half * 0.99999f) continue;
-        if (plain && d + lo == x[e] && x[e] - d == lo) {
-          const bool odd = (unsigned)code[e] & 1u;
-          if (off > half || (off == half && odd)) code[e] += rest[e] > 0.0f ? 1.0f : -1.0f;
-        } else {
-          const double c = step > 0.0f ? rint(((double)x[e] - (double)lo) / (double)step) : 0.0;
-          code[e] = (float)fmin(fmax(c, 0.0), 15.0);
-        }
+      for (int e = 0; e < 4; ++e) {
+        x[p][2 * e] = F32 ? word_float(w[i][p][F32 ? e / 2 : 0][(2 * e) & 3]) : bf16_lo(w[i][p][0][e]);
+        x[p][2 * e + 1] = F32 ? word_float(w[i][p][F32 ? e / 2 : 0][(2 * e + 1) & 3]) : bf16_hi(w[i][p][0][e]);
+        mn = fminf(fminf(mn, x[p][2 * e]), x[p][2 * e + 1]);
+        mx = fmaxf(fmaxf(mx, x[p][2 * e]), x[p][2 * e + 1]);
+        if (!F32) least = fminf(fminf(least, fabsf(x[p][2 * e])), fabsf(x[p][2 * e + 1]));
       }
     }
-    unsigned packed = 0;
+    mn = fminf(mn, lane_dpp<0xB1>(mn)); mx = fmaxf(mx, lane_dpp<0xB1>(mx));
+    mn = fminf(mn, lane_dpp<0x4E>(mn)); mx = fmaxf(mx, lane_dpp<0x4E>(mx));
+    // (least stays the lane's: it is asked about the lane's elements)
+    const unsigned lo_bits = bf16_below(mn);
+    const float lo = word_float(lo_bits);
+    const unsigned step_bits = step_of(mx, lo);
+    const float step = word_float(step_bits);
+    // A code is the quotient (x - lo) / step rounded to even, and one in 340 of normal bf16 elements is a true tie.  bf16: where neither lo
+    // nor an element of the lane is below 2^-15 of the largest magnitude, x - lo is exact in float, a quotient that is
+    // representable comes out exact after one correction, and one that is no tie keeps 2^-20.1 from it, more than its rounding
+    // error, 2^-21.  Otherwise, and for float, a code is judged by what it leaves: rests next to half a step are looked at once more, in
+    // double where x - lo was rounded; so are steps whose reciprocal or range leaves the float range.  (A code plus kWhole is
+    // rounded to a whole number and sits in the float's low bits.)
+    constexpr float kWhole = 12582912.0f;
+    const float inv = __builtin_amdgcn_rcpf(step), half = 0.5f * step;
+    float whole[PIECES][8], far = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) packed |= ((unsigned)code[e] & 15u) << (4 * e);
+    for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float d = x[p][e] - lo, q = d * inv;
+        whole[p][e] = fmaf(fmaf(-q, step, d), inv, q) + kWhole;
+        if (F32) far = fmaxf(far, fabsf(fmaf(kWhole - whole[p][e], step, d)));
+      }
+    const bool plain = step > 1e-25f && step < 1e30f;
+    if (!F32 && lo != 0.0f) least = fminf(least, fabsf(lo));
+    if (!plain || (F32 ? far > half * 0.99999f : least < fmaxf(fabsf(lo), fabsf(mx)) * 0x1p-15f)) {
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float d = x[p][e] - lo, rest = fmaf(kWhole - whole[p][e], step, d), off = fabsf(rest);
+          if (plain && off <= half * 0.99999f) continue;
+          if (plain && d + lo == x[p][e] && x[p][e] - d == lo) {
+            const bool odd = __builtin_bit_cast(unsigned, whole[p][e]) & 1u;
+            if (off > half || (off == half && odd)) whole[p][e] += rest > 0.0f ? 1.0f : -1.0f;
+          } else {
+            const double c = step > 0.0f ? rint(((double)x[p][e] - (double)lo) / (double)step) : 0.0;
+            whole[p][e] = (float)fmin(fmax(c, 0.0), 15.0) + kWhole;
+          }
+        }
+    }
     if (!u[i].live) continue;
     char* dst = a.cache[kv] + (long long)u[i].slot * a.cache_stride;
-    *(unsigned*)(dst + u[i].g * 32 + sub * 4) = packed;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      // sum of bits(code + kWhole) << 4e: what kWhole's own bits add is known
+      unsigned packed = __builtin_bit_cast(unsigned, whole[p][7]);
+#pragma unroll
+      for (int e = 6; e >= 0; --e) packed = (packed << 4) + __builtin_bit_cast(unsigned, whole[p][e]);
+      packed -= 0x4B400000u + (0x4B400000u << 4) + (0x4B400000u << 8);
+      *(unsigned*)(dst + u[i].g * 32 + (p * LANES + sub) * 4) = packed;
+    }
     if (sub == 0) *(unsigned*)(dst + codes + (long long)u[i].g * 4) = (lo_bits >> 16) | step_bits;
   }
 }
 
+constexpr int kQ4Units = 4;
 template <bool F32>
 __global__ __launch_bounds__(256) void k_q4_load(Q4CopyArgs a) {
   const int kv = blockIdx.y, sub = threadIdx.x & 7;
@@ -145,7 +177,7 @@ __global__ __launch_bounds__(256) void k_q4_load(Q4CopyArgs a) {
   const int groups = a.heads * (a.D / kQ4Group);
   const long long codes = q4_code_bytes(a.heads, a.D);
   Q4Unit u[kQ4Units];
-  q4_units(a, groups, u);
+  q4_units<8, kQ4Units>(a, groups, u);
   unsigned packed[kQ4Units], pair[kQ4Units];
 #pragma unroll
   for (int i = 0; i < kQ4Units; ++i) {
@@ -683,7 +715,7 @@ hipError_t launch_q4_attn(const Q4AttnArgs& a, hipStream_t s) {
 }
 
 dim3 q4_copy_grid(const Q4CopyArgs& a) {
-  const long long units = a.n * a.heads * (a.D / kQ4Group), each = 32 * kQ4Units;
+  const long long units = a.n * a.heads * (a.D / kQ4Group), each = kQ4Block;
   return dim3((unsigned)((units + each - 1) / each), 2);
 }
 

@@ -529,6 +529,64 @@ def test_eviction(lengths, budget, n_sink, n_recent, page, row_bytes, kind):
 
 
 # ----------------------------------------------------------------------------- all of them, as they are used
+def test_cache_copies_and_a_long_eviction_replayed_from_a_graph():
+    _say("graph: rows into the cache, a long eviction, rows out of it")
+    rng = np.random.default_rng(31)
+    heads, D, page, lengths, budget = 4, 64, 64, [25000, 700, 0], 7000
+    R, most, row = len(lengths), max(lengths), up.uniprefill_q4_row_bytes(heads, D)
+    kept = [min(n, budget) for n in lengths]
+    need, new = [-(-n // page) for n in lengths], [-(-n // page) for n in kept]
+    table, new_table = np.full((R, max(need)), -1, np.int32), np.full((R, max(new)), -1, np.int32)
+    pages, at = rng.permutation(sum(need) + sum(new)), 0
+    for t, counts in ((table, need), (new_table, new)):
+        for r, n in enumerate(counts):
+            t[r, :n] = pages[at:at + n]
+            at += n
+    slots = np.concatenate([ao.page_rows(table[r], n, page) for r, n in enumerate(lengths)])
+    out_slots = np.concatenate([ao.page_rows(new_table[r], n, page) for r, n in enumerate(kept)])
+    p = up.make_params(num_seqs=R, total_tokens=sum(lengths), block_size=64, num_q_heads=heads, num_kv_heads=heads, head_dim=D)
+    n, m = len(slots), len(out_slots)
+    k = torch.zeros(n, heads, D, dtype=BF, device="cuda")
+    cache = torch.zeros(at * page, row, dtype=torch.uint8, device="cuda")
+    mass = torch.zeros(R, most, device="cuda")
+    kept_idx, mass_out = torch.zeros(R, budget, dtype=torch.int32, device="cuda"), torch.zeros(R, budget, device="cuda")
+    new_len, back = torch.zeros(R, dtype=torch.int32, device="cuda"), torch.zeros(m, heads, D, dtype=BF, device="cuda")
+    lens, tab, new_tab, s_in, s_out = (_dev(np.asarray(a)) for a in (np.array(lengths, np.int32), table, new_table, slots, out_slots))
+
+    def calls():
+        up.uniprefill_cache_store_q4(p, k, None, heads * D, s_in, n, None, cache, None, row, at * page)
+        up.uniprefill_cache_evict(cache, None, row, row, mass, most, lens, R, most, budget, 5, 64, tab, table.shape[1], new_tab,
+                                  new_table.shape[1], page, kept_idx, mass_out, budget, new_len)
+        up.uniprefill_cache_load_q4(p, cache, None, row, at * page, s_out, m, None, back, None, heads * D)
+
+    calls()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    for _ in range(4):
+        rows, rows64 = _rows(rng, BF, n, heads, D)
+        masses = rng.random((R, most)).astype(np.float32)
+        k.copy_(rows)
+        mass.copy_(torch.from_numpy(masses))
+        back.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        a = b = 0
+        for r, length in enumerate(lengths):
+            stay = ao.evict_tokens(masses[r], length, budget, 5, 64)
+            np.testing.assert_array_equal(kept_idx[r, :len(stay)].cpu().numpy(), stay)
+            np.testing.assert_array_equal(mass_out[r, :len(stay)].cpu().numpy(), masses[r][stay])
+            want = ao.q4_values(*ao.q4_quantise(rows[a:a + length].float().numpy()[stay])) if length else np.zeros((0, heads, D))
+            got = back[b:b + len(stay)].double().cpu().numpy()
+            assert (np.abs(got - want) <= (2.0 ** -8 + F) * np.abs(want)).all()      # to float, then to bf16
+            a, b = a + length, b + len(stay)
+        first = [t.clone() for t in (kept_idx, mass_out, new_len, back)]
+        calls()
+        torch.cuda.synchronize()
+        for x, y in zip(first, (kept_idx, mass_out, new_len, back)):
+            assert torch.equal(x, y)
+
+
 def test_prompt_drop_cache_decode_evict_decode():
     """A layer's attention hands its log-sum-exp to the drop; the kept tokens' keys and values enter the 4-bit cache;
     three decode steps read it and accumulate weights; the cache shrinks and decoding goes on."""
