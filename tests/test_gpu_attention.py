@@ -303,6 +303,26 @@ def test_rows_enter_and_leave_the_cache(n, heads, D, dtype):
         assert (got[n:] == -7.0).all() and (got[:, heads * D:] == -7.0).all()
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("kind", ["plain", "coarse", "shifted", "whole_numbers", "tiny_lowest", "no_negatives", "tiny_beside_large", "powers"])
+def test_codes_next_to_ties_and_rounded_differences(kind, dtype):
+    """Bit for bit the oracle's bytes where quotients are ties or nearly, and where x - lowest is not a float."""
+    _say("4-bit codes", kind, dtype)
+    rng = np.random.default_rng(len(kind))
+    n, heads, D = 512, 4, 128
+    x = rng.standard_normal((n, heads, D)).astype(np.float32)
+    small = np.float32(2.0) ** rng.integers(-30, -10, x.shape)
+    x = {"plain": x, "coarse": np.round(x * 4) / 4, "shifted": x + 100, "whole_numbers": rng.integers(-8, 9, x.shape),
+         "tiny_lowest": np.where(np.arange(D) % 64 == 17, small, np.abs(x) + 1), "no_negatives": np.maximum(x, 0),
+         "tiny_beside_large": np.where(rng.random(x.shape) < 0.1, x * small, x), "powers": small * np.sign(x)}[kind]
+    t = torch.from_numpy(np.asarray(x, np.float32)).to(dtype)
+    row = up.uniprefill_q4_row_bytes(heads, D)
+    cache = torch.zeros(n, row, dtype=torch.uint8, device="cuda")
+    up.uniprefill_cache_store_q4(_copy_params(heads, D, dtype, 0), t.cuda(), None, heads * D, _dev(np.arange(n)), n, None, cache, None, row, n)
+    torch.cuda.synchronize()
+    np.testing.assert_array_equal(cache.cpu().numpy(), ao.q4_pack(*ao.q4_quantise(t.float().numpy())))
+
+
 def test_cache_copies_stop_at_the_count_on_the_device():
     _say("4-bit store and load: device count, keys alone")
     rng = np.random.default_rng(0)
