@@ -16,7 +16,9 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // ---- attention of a packed batch
 // A work-group takes 256 rows (tokens x query heads of one kv head; 8 waves) of one sequence and walks over the
-// keys they see; 128 rows (4 waves) where work-groups of 256 would be fewer than the CUs.  Where the rows alone leave
+// keys they see; 128 rows (4 waves) where work-groups of 256 would be fewer than the CUs, or fewer than twice as many with the
+// longest well beyond a CU's share (one prompt of 2048, 32/8 heads, 67 -> 57 us, float 500 -> 296; 2048 tokens after 6000 others
+// are even and stay: 244 us, 254 in work-groups of 128).  Where the rows alone leave
 // the chip idle all the same -- decode rows and short chunks on long caches -- the keys of every row tile are cut into
 // pieces of part_keys and the pieces joined.
 struct AttnGeometry {
@@ -47,17 +49,20 @@ int attn_geometry(const Problem& pb, const int32_t* cu, const int32_t* ck, AttnG
     if (N > 0) longest = L > longest ? L : longest;
   }
   if (longest > kMaxLength) return UP_ERR_UNSUPPORTED;
-  if (live * pb.Hkv < kCUs) g->rows = 128;
-  auto tiles_of = [&](long long N) { return (N * pb.Gq + g->rows - 1) / g->rows; };
-  double work = 0;
-  for (int r = 0; r < pb.R; ++r) {
-    const long long N = cu[r + 1] - cu[r], L = ck[r + 1] - ck[r], tiles = tiles_of(N);
-    if (N > 0) work += (double)tiles * (double)(L - N) + 0.5 * (double)(tiles + 1) * (double)N;
-  }
+  auto tiles_of = [&](long long N, int rows) { return (N * pb.Gq + rows - 1) / rows; };
+  auto keys_per_cu = [&](int rows) {
+    double work = 0;
+    for (int r = 0; r < pb.R; ++r) {
+      const long long N = cu[r + 1] - cu[r], L = ck[r + 1] - ck[r], tiles = tiles_of(N, rows);
+      if (N > 0) work += (double)tiles * (double)(L - N) + 0.5 * (double)(tiles + 1) * (double)N;
+    }
+    return work * pb.Hkv / kCUs;
+  };
+  if (live * pb.Hkv < kCUs || (live * pb.Hkv < 2 * kCUs && 2.0 * (double)longest > 1.5 * keys_per_cu(128))) g->rows = 128;
+  const double fair = keys_per_cu(g->rows);
   g->parts = 1;
   g->slots = (long long)pb.T * pb.Gq / g->rows + pb.R;
   g->items = g->slots;
-  const double fair = work * pb.Hkv / kCUs;      // keys per CU
   const long long fewest = pb.qk_is_f32 ? 256 : 512;
   if ((double)longest > fair && longest > fewest) {
     const long long want = fair > 2.0 * (double)fewest ? (long long)(0.5 * fair) : fewest;
@@ -73,7 +78,7 @@ int attn_geometry(const Problem& pb, const int32_t* cu, const int32_t* ck, AttnG
       g->parts = (int)((longest + part - 1) / part);
       g->items = 0;
       for (int r = 0; r < pb.R; ++r) {
-        const long long tiles = tiles_of(cu[r + 1] - cu[r]), n = (ck[r + 1] - ck[r] + part - 1) / part;
+        const long long tiles = tiles_of(cu[r + 1] - cu[r], g->rows), n = (ck[r + 1] - ck[r] + part - 1) / part;
         g->items += tiles * n;
         if (n > 1) g->pieces += tiles * n;
       }
