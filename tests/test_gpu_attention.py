@@ -549,6 +549,55 @@ def test_eviction(lengths, budget, n_sink, n_recent, page, row_bytes, kind):
 
 
 # ----------------------------------------------------------------------------- all of them, as they are used
+def test_slots_beyond_4_gib_of_a_cache():
+    """The same calls with their pages at the front and at the far end of caches of 4.5 GiB: the same bits."""
+    _say("caches of more than 4 GiB")
+    rng = np.random.default_rng(41)
+    heads, hq, D, page, n, budget = 8, 16, 128, 16, 500, 200
+    used, new = -(-n // page), -(-budget // page)
+    mass_host = _dev(rng.random((1, n)).astype(np.float32))
+    rows = _rows(rng, BF, n, heads, D)[0].cuda()
+    q = _rows(rng, BF, 1, hq, D)[0].cuda()
+    lens = _dev(np.array([n], np.int32))
+    cu, ck = np.array([0, 1], np.int32), np.array([0, n], np.int32)
+    for stride, q4 in ((heads * D * 2, False), (up.uniprefill_q4_row_bytes(heads, D), True)):
+        pages = (9 << 29) // (stride * page)
+        cache = torch.zeros(pages * page, stride, dtype=torch.uint8, device="cuda")
+        found = []
+        for first in (0, pages - used - new):
+            order = first + rng.permutation(used + new)
+            table, new_table = order[None, :used].astype(np.int32), order[None, used:].astype(np.int32)
+            slots = ao.page_rows(table[0], n, page)
+            p = up.make_params(num_seqs=1, total_tokens=1, block_size=64, num_q_heads=hq, num_kv_heads=heads, head_dim=D)
+            out, lse = torch.zeros(1, hq * D, dtype=BF, device="cuda"), torch.zeros(hq, 1, device="cuda")
+            tab, new_tab = _dev(table), _dev(new_table)
+            ws = torch.zeros(1 << 24, dtype=torch.uint8, device="cuda")
+            if q4:
+                up.uniprefill_cache_store_q4(p, rows, rows, heads * D, _dev(slots), n, None, cache, cache, stride, pages * page)
+                up.uniprefill_attention_q4(p, q, cache, cache, stride, lens, n, tab, used, page, out, hq * D, lse, 1, None, None, 0, ws,
+                                           ws.numel())
+            else:
+                cache[_dev(slots)] = rows.view(torch.uint8).reshape(n, stride)
+                up.uniprefill_attention(p, q, cache, cache, heads * D, _dev(cu), cu, _dev(ck), ck, tab, used, page, out, hq * D, lse, 1,
+                                        ws, ws.numel())
+            kept_idx, mass_out = torch.zeros(1, budget, dtype=torch.int32, device="cuda"), torch.zeros(1, budget, device="cuda")
+            new_len = torch.zeros(1, dtype=torch.int32, device="cuda")
+            up.uniprefill_cache_evict(cache, None, stride, stride, mass_host, n, lens, 1, n, budget, 4, 4, tab, used, new_tab, new,
+                                      page, kept_idx, mass_out, budget, new_len)
+            torch.cuda.synchronize()
+            moved = cache[_dev(ao.page_rows(new_table[0], budget, page))]
+            assert torch.equal(moved, cache[_dev(slots)][kept_idx[0].long()]) and moved.any()
+            back = torch.zeros(n, heads * D, dtype=BF, device="cuda")
+            if q4:
+                up.uniprefill_cache_load_q4(p, cache, None, stride, pages * page, _dev(slots), n, None, back, None, heads * D)
+                torch.cuda.synchronize()
+            found.append((out, lse, kept_idx, mass_out, moved, back))
+        for a, b in zip(*found):
+            assert torch.equal(a, b)
+        assert found[0][0].any()
+        del cache, found
+
+
 def test_cache_copies_and_a_long_eviction_replayed_from_a_graph():
     _say("graph: rows into the cache, a long eviction, rows out of it")
     rng = np.random.default_rng(31)
