@@ -229,6 +229,13 @@ def _graph(call):
     return g
 
 
+def test_calls_without_a_stream_go_to_the_current_one():
+    from paper_2605_06221_amd import binding
+    for side in (torch.cuda.default_stream(), torch.cuda.Stream(), torch.cuda.Stream()):
+        with torch.cuda.stream(side):
+            assert (binding._stream(None).value or 0) == side.cuda_stream
+
+
 def test_attention_and_decode_replayed_from_a_graph():
     _say("graphs: attention in pieces, decode with masses, two graphs in turn on one workspace each")
     b = Batch(12, [1, 300], 8, 2, 128, earlier=[5000, 0])
