@@ -178,9 +178,15 @@ def test_attention_with_the_keys_cut_into_pieces(lengths, earlier, hq, hkv, D, d
     ([2100, 1, 67], None, 32, 8, 128, BF, 0), ([1100], [333], 64, 8, 64, BF, 16), ([700, 0, 400], [50, 0, 0], 64, 8, 256, BF, 8),
     ([1010], [129], 64, 16, 128, F32, 24), ([1010, 1], [3, 2500], 64, 16, 64, F32, 7), ([2100, 1], [0, 30000], 32, 8, 128, BF, 16),
     ([1050, 3], [0, 9000], 64, 8, 64, BF, 0), ([1050, 2], [100, 5000], 64, 16, 256, BF, 5),
+    # two rounds and more
+    ([300], [700], 512, 8, 128, BF, 16), ([520, 1, 67], None, 256, 16, 64, BF, 0), ([600, 0, 30], [40, 0, 9000], 256, 16, 256, BF, 8),
+    ([530], [129], 256, 16, 128, F32, 24), ([530, 1], [3, 2500], 256, 16, 64, F32, 7), ([1100], None, 128, 32, 128, BF, 0),
+    ([540, 2], [100, 5000], 256, 16, 256, BF, 5), ([270, 1], [0, 30000], 512, 8, 64, BF, 128), ([515], None, 256, 16, 128, F32, 0),
+    ([515], None, 256, 16, 64, F32, 0), ([515], None, 256, 16, 256, BF, 0), ([140, 140], [2000, 1999], 512, 8, 128, BF, 0),
 ])
 def test_attention_in_work_groups_of_256_rows(lengths, earlier, hq, hkv, D, dtype, page):
-    """Batches with at least as many tiles of 256 rows as the chip has CUs take eight waves per work-group."""
+    """Batches with at least as many tiles of 256 rows as the chip has CUs: eight waves per work-group, or four where one round of them
+    would be uneven."""
     _say("attention, large", lengths, earlier, hq, hkv, D, dtype, page)
     assert sum(-(-n * (hq // hkv) // 256) for n in lengths) * hkv >= 256
     b = Batch(31, lengths, hq, hkv, D, dtype, earlier=earlier, page=page)
@@ -556,6 +562,49 @@ def test_eviction(lengths, budget, n_sink, n_recent, page, row_bytes, kind):
 
 
 # ----------------------------------------------------------------------------- all of them, as they are used
+def test_eviction_clamps_lengths_of_the_device():
+    _say("eviction: lengths out of range")
+    rng = np.random.default_rng(51)
+    n, budget, page = 600, 100, 32
+    table = np.arange(3 * 19, dtype=np.int32).reshape(3, 19)
+    new_table = 57 + np.arange(3 * 4, dtype=np.int32).reshape(3, 4)
+    before = rng.integers(0, 256, (69 * page, 48)).astype(np.uint8)
+    cache, mass = _dev(before), rng.random((3, n)).astype(np.float32)
+    kept_idx, mass_out = torch.full((3, budget), -77, dtype=torch.int32, device="cuda"), torch.full((3, budget), -7.0, device="cuda")
+    new_len = torch.full((3,), -77, dtype=torch.int32, device="cuda")
+    up.uniprefill_cache_evict(cache, None, 48, 48, _dev(mass), n, _dev(np.array([1 << 30, -5, 70], np.int32)), 3, n, budget, 8, 8, _dev(table), 19,
+                              _dev(new_table), 4, page, kept_idx, mass_out, budget, new_len)
+    torch.cuda.synchronize()
+    assert new_len.tolist() == [100, 0, 70] and (kept_idx[1] == -77).all() and (kept_idx[2, 70:] == -77).all()
+    want = before.copy()
+    for r, length in ((0, n), (2, 70)):
+        stay = ao.evict_tokens(mass[r], length, budget, 8, 8)
+        np.testing.assert_array_equal(kept_idx[r, :len(stay)].cpu().numpy(), stay)
+        want[ao.page_rows(new_table[r], len(stay), page)] = before[ao.page_rows(table[r], length, page)[stay]]
+    np.testing.assert_array_equal(cache.cpu().numpy(), want)
+
+
+def test_calls_at_the_same_time_on_two_streams():
+    """Two batches, two workspaces, two streams, nothing between the calls: the results of each alone."""
+    _say("two streams at once")
+    work = [Batch(61, [900, 70], 8, 2, 128, earlier=[3000, 0], page=16), Batch(62, [1, 1, 1], 32, 8, 128, earlier=[9000, 5000, 20]),
+            Decode(63, [5000, 30, 700], 32, 8, 128, mass=True), Decode(64, [300] * 20, 8, 4, 64, mass=True)]
+    alone = []
+    for w in work:
+        w.run()
+        w.check()
+        alone.append([t.clone() for t in (w.out, w.lse) + ((w.mass_out,) if isinstance(w, Decode) else ())])
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for i in range(10):
+        for j, w in enumerate(work):
+            w.run(stream=streams[j % 2])
+    torch.cuda.synchronize()
+    for w, want in zip(work, alone):
+        for a, b in zip((w.out, w.lse) + ((w.mass_out,) if isinstance(w, Decode) else ()), want):
+            assert torch.equal(a, b)
+
+
 def test_slots_beyond_4_gib_of_a_cache():
     """The same calls with their pages at the front and at the far end of caches of 4.5 GiB: the same bits."""
     _say("caches of more than 4 GiB")
