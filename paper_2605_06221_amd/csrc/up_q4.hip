@@ -253,8 +253,9 @@ struct Q4Cut {      // total steps among at most `groups` work-groups: the first
 };
 
 struct Q4Run { int r, len; unsigned from, to, seq_first; };      // steps from .. to, beginning in sequence r
+// own_len: the length of sequence threadIdx.x, asked for before.
 template <int THREADS>
-__device__ __forceinline__ bool q4_run(const Q4AttnArgs& a, int step_keys, unsigned* sm, Q4Run& run) {
+__device__ __forceinline__ bool q4_run(const Q4AttnArgs& a, int step_keys, int own_len, unsigned* sm, Q4Run& run) {
   constexpr int WAVES = THREADS / 64;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const bool notes = blockIdx.x == 0 && blockIdx.z == 0;
@@ -265,7 +266,7 @@ __device__ __forceinline__ bool q4_run(const Q4AttnArgs& a, int step_keys, unsig
     unsigned before = 0;
     for (int c = 0; c < chunks; ++c) {
       const int r = c * THREADS + tid;
-      const int len = r < a.R ? imin(imax(a.kv_len[r], 0), a.max_len) : 0;
+      const int len = r < a.R ? imin(imax(c == 0 ? own_len : a.kv_len[r], 0), a.max_len) : 0;
       const unsigned n = (unsigned)(len + step_keys - 1) / (unsigned)step_keys;
       unsigned sum = n;
 #pragma unroll
@@ -317,7 +318,7 @@ __global__ __launch_bounds__(64 * q4_waves(D), q4_dense(D)) void k_q4_attn(Q4Att
   constexpr int SWAP = HP - 1 < 3 ? HP - 1 : 3;
   constexpr int DT = D / 16;
   constexpr int PLACES = kQ4Places<D>;
-  constexpr int LOADS = (2 * PLACES + W - 1) / W;      // loads of a wave per step
+  constexpr int LOADS = (PLACES + W - 1) / W;          // loads of a wave per step and cache
   // (two variables per buffer: see the attention of packed batches)
   __shared__ __align__(16) u32x4 k0s[64 * PLACES], k1s[64 * PLACES], v0s[64 * PLACES], v1s[64 * PLACES];
   __shared__ __align__(16) f32x2 spair[W][NG][kQ4Wave];      // (step, offset) of a wave's keys: K's times c, then V's
@@ -335,9 +336,26 @@ __global__ __launch_bounds__(64 * q4_waves(D), q4_dense(D)) void k_q4_attn(Q4Att
   const CodeBits bits = code_bits();
   const int step_keys = kQ4Wave * a.wave_parts;
 
+  // ---- staging.  A row in LDS: the codes of the work-group's heads (permuted pieces), then their pairs.  Load i of this wave
+  // writes 64 consecutive pieces; where its lane's piece comes from inside which row does not change from step to step, nor from
+  // K's row to V's
+  const int own_len = a.kv_len[imin(tid, a.R - 1)];
+  const int code_places = heads * HP, places = code_places + (heads * NG * 4 + 15) / 16;
+  const int loads = a.wave_parts * places;      // per cache
+  const unsigned places_magic = 0xFFFFFFFFu / (unsigned)places;
+  int from_row[LOADS], from_at[LOADS];
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    unsigned row, place;
+    divmod_by((unsigned)((i * W + wave) * 64 + lane), (unsigned)places, places_magic, row, place);
+    from_row[i] = (int)row;
+    from_at[i] = (int)place < code_places ? head0 * (D / 2) + (int)(place ^ ((row >> 2) & SWAP)) * 16
+                                     : (int)q4_code_bytes(a.Hkv, D) + head0 * NG * 4 + ((int)place - code_places) * 16;
+  }
+
   // ---- this work-group's run of steps
   Q4Run run;
-  if (!q4_run<THREADS>(a, step_keys, (unsigned*)rows1, run)) return;
+  if (!q4_run<THREADS>(a, step_keys, own_len, (unsigned*)rows1, run)) return;
   int r = run.r;
 
   u32x4 qf[NG][2];
@@ -368,29 +386,16 @@ __global__ __launch_bounds__(64 * q4_waves(D), q4_dense(D)) void k_q4_attn(Q4Att
   float m, l, ol[NG];                           // reference, sum of weights, sum of weights * offsets
   int len = 0, first = 0, last = 0;             // the sequence's length; its keys that this work-group takes
 
-  // ---- staging.  A row in LDS: the codes of the work-group's heads (permuted pieces), then their pairs.  Load i of this wave
-  // writes 64 consecutive pieces; where its lane's piece comes from inside which row does not change from step to step
-  const int code_places = heads * HP, places = code_places + (heads * NG * 4 + 15) / 16;
-  const int loads = a.wave_parts * places;      // per cache
-  const unsigned places_magic = 0xFFFFFFFFu / (unsigned)places;
-  int from_row[LOADS], from_at[LOADS];
-#pragma unroll
-  for (int i = 0; i < LOADS; ++i) {
-    const int j = i * W + wave, p = (j >= loads ? j - loads : j) * 64 + lane;
-    unsigned row, place;
-    divmod_by((unsigned)p, (unsigned)places, places_magic, row, place);
-    from_row[i] = (int)row;
-    from_at[i] = (int)place < code_places ? head0 * (D / 2) + (int)(place ^ ((row >> 2) & SWAP)) * 16
-                                     : (int)q4_code_bytes(a.Hkv, D) + head0 * NG * 4 + ((int)place - code_places) * 16;
-  }
   auto stage = [&](const long long* rows, u32x4* sk, u32x4* sv) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
       const int j = i * W + wave;
-      if (j < 2 * loads) {
-        const char* src = (j >= loads ? a.v : a.k) + rows[from_row[i]] + from_at[i];
-        u32x4* dst = j >= loads ? sv + (j - loads) * 64 : sk + j * 64;
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+      if (j < loads) {
+        const long long at = rows[from_row[i]] + from_at[i];
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(a.k + at),
+                                         (__attribute__((address_space(3))) void*)(sk + j * 64), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(a.v + at),
+                                         (__attribute__((address_space(3))) void*)(sv + j * 64), 16, 0, 0);
       }
     }
   };
