@@ -357,6 +357,7 @@ int uniprefill_cache_evict(void* k_cache, void* v_cache, int64_t row_bytes, int6
   if (!aligned_to(mass, 4) || !aligned_to(mass_out, 4) || !aligned_to(kept_idx, 4) || !aligned_to(kv_len_dev, 4) || !aligned_to(new_len, 4))
     return UP_ERR_ALIGN;
   if (num_seqs > 65535 || max_kv_len > kMaxLength || most > (INT32_MAX - 1024) / (row_bytes / 16)) return UP_ERR_UNSUPPORTED;
+  if (max_kv_len > 0 && ((const void*)mass == mass_out || (const void*)kept_idx == mass_out || (const void*)mass == kept_idx)) return UP_ERR_UNSUPPORTED;
   EvictArgs a{};
   a.k = (char*)k_cache; a.v = (char*)v_cache; a.row_bytes = row_bytes; a.cache_stride = cache_row_stride;
   a.mass = mass; a.mass_out = mass_out; a.mass_stride = mass_row_stride; a.mass_out_stride = mass_out_stride;

@@ -195,3 +195,9 @@ def test_refusals_of_what_the_kernels_cannot_count():
     # more 16-byte pieces of kept rows than are counted in 31 bits
     assert _evict(max_len=1 << 30, mass_stride=1 << 30, tstride=1 << 30, budget=1 << 30, out_stride=1 << 30, nstride=1 << 30, row=64,
                   stride=64) == up.UP_ERR_UNSUPPORTED
+
+
+def test_evict_refuses_masses_in_place():
+    other = dict(kept=A + 4096, mass_out=A + 8192)
+    for same in (dict(other, mass_out=A), dict(other, kept=A), dict(other, kept=A + 8192)):
+        assert _evict(**same) == up.UP_ERR_UNSUPPORTED
