@@ -356,7 +356,8 @@ int uniprefill_cache_evict(void* k_cache, void* v_cache, int64_t row_bytes, int6
   if ((st = check_table(new_table, new_table_stride, kv_block_size, most)) != UP_OK) return st;
   if (!aligned_to(mass, 4) || !aligned_to(mass_out, 4) || !aligned_to(kept_idx, 4) || !aligned_to(kv_len_dev, 4) || !aligned_to(new_len, 4))
     return UP_ERR_ALIGN;
-  if (num_seqs > 65535 || max_kv_len > kMaxLength || most > (INT32_MAX - 1024) / (row_bytes / 16)) return UP_ERR_UNSUPPORTED;
+  // (the kernels count 16-byte pieces in 31 bits, those of one row too where max_kv_len leaves no rows)
+  if (num_seqs > 65535 || max_kv_len > kMaxLength || imax(most, 1) > (INT32_MAX - 1024) / (row_bytes / 16)) return UP_ERR_UNSUPPORTED;
   if (max_kv_len > 0 && ((const void*)mass == mass_out || (const void*)kept_idx == mass_out || (const void*)mass == kept_idx)) return UP_ERR_UNSUPPORTED;
   EvictArgs a{};
   a.k = (char*)k_cache; a.v = (char*)v_cache; a.row_bytes = row_bytes; a.cache_stride = cache_row_stride;

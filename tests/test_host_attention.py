@@ -201,3 +201,10 @@ def test_evict_refuses_masses_in_place():
     other = dict(kept=A + 4096, mass_out=A + 8192)
     for same in (dict(other, mass_out=A), dict(other, kept=A), dict(other, kept=A + 8192)):
         assert _evict(**same) == up.UP_ERR_UNSUPPORTED
+
+
+def test_evict_of_no_tokens_with_rows_beyond_what_is_counted():
+    # max_kv_len 0: no row is moved, and a row's 16-byte pieces still have to fit 31 bits
+    for pieces in ((1 << 31) - 1024, 1 << 32):
+        assert _evict(max_len=0, row=16 * pieces, stride=16 * pieces, table=None, new=None, mass=None, kept=None,
+                      mass_out=None) == up.UP_ERR_UNSUPPORTED
