@@ -8,6 +8,9 @@
 namespace up {
 
 // --- causal attention of a packed batch
+// pieces of part_keys keys that `keys` keys are cut into (both below 2^31: their sum leaves an int, not 32 bits)
+UP_HD int attn_pieces(int keys, int part_keys) { return (int)(((unsigned)keys + (unsigned)part_keys - 1u) / (unsigned)part_keys); }
+
 struct AttnArgs {
   const char* q;
   const char* k;

@@ -136,9 +136,9 @@ __device__ __forceinline__ bool attn_locate(const AttnArgs& a, int item, AttnIte
     long long ni = 0, np = 0;
     int parts = 1;
     if (r < a.R) {
-      const long long N = a.cu[r + 1] - a.cu[r], L = a.cu_k[r + 1] - a.cu_k[r];
+      const long long N = a.cu[r + 1] - a.cu[r];
       const long long tiles = (N * a.Gq + ROWS - 1) / ROWS;
-      parts = (int)((L + a.part_keys - 1) / a.part_keys);
+      parts = attn_pieces(a.cu_k[r + 1] - a.cu_k[r], a.part_keys);
       ni = tiles * parts;
       np = parts > 1 ? ni : 0;
     }
@@ -479,7 +479,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
   const int nrow = rows_left < a.rows ? (int)rows_left : a.rows;
   const int tok0 = (int)(row0 / a.Gq), rem0 = (int)(row0 % a.Gq);
   const int visible = Lk - N + tok0 + (rem0 + nrow - 1) / a.Gq + 1;
-  const int parts = (visible + a.part_keys - 1) / a.part_keys;      // pieces that saw a key
+  const int parts = attn_pieces(visible, a.part_keys);      // pieces that saw a key
   constexpr int PER = D / 64;
   for (int x = blockIdx.y * 4 + wave; x < nrow; x += gridDim.y * 4) {
     const long long step = (long long)a.Hkv * a.rows, at0 = ((long long)first * a.Hkv + kvh) * a.rows + x;

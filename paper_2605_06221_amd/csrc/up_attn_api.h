@@ -69,16 +69,16 @@ int attn_geometry(const Problem& pb, const int32_t* cu, const int32_t* ck, AttnG
     const long long part = (want + 127) / 128 * 128;
     double rows = 0;      // rows of float sums that the pieces leave
     for (int r = 0; r < pb.R; ++r) {
-      const long long N = cu[r + 1] - cu[r], n = (ck[r + 1] - ck[r] + part - 1) / part;
+      const long long N = cu[r + 1] - cu[r], n = attn_pieces(ck[r + 1] - ck[r], (int)part);
       if (n > 1) rows += (double)(N * pb.Hq) * (double)n;
     }
     const double gain = ((double)longest - fair - (double)part) * attn_key_us(pb.qk_is_f32, D) * g->rows / 128, cost = 6.0 + rows * D * 8.0 / 3e6;
     if (part < longest && gain > cost) {
       g->part_keys = (int)part;
-      g->parts = (int)((longest + part - 1) / part);
+      g->parts = attn_pieces((int)longest, (int)part);
       g->items = 0;
       for (int r = 0; r < pb.R; ++r) {
-        const long long tiles = tiles_of(cu[r + 1] - cu[r], g->rows), n = (ck[r + 1] - ck[r] + part - 1) / part;
+        const long long tiles = tiles_of(cu[r + 1] - cu[r], g->rows), n = attn_pieces(ck[r + 1] - ck[r], (int)part);
         g->items += tiles * n;
         if (n > 1) g->pieces += tiles * n;
       }
