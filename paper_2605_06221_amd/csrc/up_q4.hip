@@ -192,6 +192,16 @@ __global__ __launch_bounds__(256) void k_q4_load(Q4CopyArgs a) {
     float x[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = fmaf((float)((packed[i] >> (4 * e)) & 15u), step, lo);
+    // bf16: rounding the float rounds the value itself once, for the float is exact or no bf16 number or middle between two lies
+    // between them, but for a lo below step / 2^12, which a float may lose.  With 2^e the power of two at or below step, code * step is a
+    // multiple of 2^(e-7), and where bf16 decides next to it are multiples of 2^(e-8) (below a power of two: of 2^(e-9)).  Any lo of
+    // the same sign below 2^(e-9) then rounds alike, step / 2^10 among them, and with that one the float is exact.
+    const float least = step * 0x1p-10f;
+    if (!F32 && fabsf(lo) < least && lo != 0.0f) {
+      const float lo2 = copysignf(least, lo);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = x[e] == lo ? lo : fmaf((float)((packed[i] >> (4 * e)) & 15u), step, lo2);
+    }
     char* dst = a.rows_out[kv] + (long long)u[i].t * a.row_stride_b[kv] + (u[i].g * 8 + sub) * (F32 ? 32 : 16);
     if (F32) {
       __builtin_nontemporal_store(f32x4{x[0], x[1], x[2], x[3]}, (f32x4*)dst);

@@ -1,11 +1,13 @@
 """GPU tests of the attention layer's operators where lengths, launches and roundings come to their ends."""
 import math
+from fractions import Fraction
 
 import numpy as np
 import pytest
 import torch
 
 import paper_2605_06221_amd as up
+from oracle import attention_oracle as ao
 from test_gpu_attention import BF, F, F32, _dev, _say
 
 pytestmark = pytest.mark.gpu
@@ -35,3 +37,45 @@ def test_one_token_after_the_longest_context():
     torch.cuda.synchronize()
     assert torch.equal(out.cpu()[0], column.to(BF))
     assert abs(float(lse) - math.log(n)) <= pieces * F + 8 * F * math.log(n)
+
+
+def _nearest(x, bits):
+    """The number of `bits` significant bits next to the rational x, ties to even (no subnormals)."""
+    if x == 0:
+        return 0.0
+    e = abs(x.numerator).bit_length() - x.denominator.bit_length()
+    while abs(x) >= Fraction(2) ** (e + 1):
+        e += 1
+    while abs(x) < Fraction(2) ** e:
+        e -= 1
+    return float(round(x / Fraction(2) ** (e - bits + 1)) * Fraction(2) ** (e - bits + 1))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_values_leave_the_cache_rounded_once(dtype):
+    """lowest + step * code in rational numbers, rounded to the type, bit for bit: pairs of all distances, whose sums lie next to the
+    middle between two bf16 numbers in many places."""
+    _say("4-bit load: rounded once", dtype)
+    rng = np.random.default_rng(3)
+    n, heads, D = 64, 2, 128
+    groups = (n, heads, D // 64)
+    sig = lambda: 1 + rng.integers(0, 128, groups) / 128.0
+    step = sig() * 2.0 ** rng.integers(-3, 4, groups)
+    lo = sig() * 2.0 ** rng.integers(-45, 46, groups) * rng.choice([-1, 1], groups)
+    step[:4], lo[:4] = 1 + 2.0 ** -7, np.array([-2.0 ** -40, 2.0 ** -40, 0.0, -1.0]).reshape(4, 1, 1)      # 3 * step is a middle
+    step[4] = 0.0
+    lo[5:8], step[5:8] = -1 - 2.0 ** -7, np.array([2.0 ** -8, 2.0 ** -9, 2.0 ** -30]).reshape(3, 1, 1)
+    code = rng.integers(0, 16, (n, heads, D)).astype(np.uint8)
+    code[:8, :, 0::16], code[:8, :, 1::16] = 3, 1
+    rows = ao.q4_pack(code, lo, step)
+    values = [[Fraction(float(lo[i, h, d // 64])) + Fraction(float(step[i, h, d // 64])) * int(code[i, h, d]) for d in range(D)]
+              for i in range(n) for h in range(heads)]
+    want = torch.tensor([[_nearest(x, 8 if dtype == BF else 24) for x in row] for row in values], dtype=torch.float64).reshape(n, heads, D)
+    twice = torch.tensor([[_nearest(Fraction(_nearest(x, 24)), 8) for x in row] for row in values], dtype=torch.float64).reshape(n, heads, D)
+    assert dtype == F32 or (twice != want).sum() > 20      # places where a detour over float shows
+    out = torch.zeros(n, heads, D, dtype=dtype, device="cuda")
+    p = up.make_params(num_seqs=1, total_tokens=1, block_size=64, num_q_heads=heads, num_kv_heads=heads, head_dim=D,
+                       qk_dtype=up.UP_F32 if dtype == F32 else up.UP_BF16)
+    up.uniprefill_cache_load_q4(p, _dev(rows), None, rows.shape[1], n, _dev(np.arange(n)), n, None, out, None, heads * D)
+    torch.cuda.synchronize()
+    assert torch.equal(out.double().cpu(), want)
