@@ -480,9 +480,11 @@ int uniprefill_fused_top_p_chunked(const up_params* p, const void* q, const void
  * k_row_stride, softmax_scale and qk_dtype (the drop layer's parameters may be
  * handed over as they are).  Query, key and value rows must be finite where a
  * token reads them; what lies beyond the sequences is never read into a result.
- * UP_ERR_UNSUPPORTED: batches of more than 2^31 - 1 work items, sequences (max_kv_len) of more than
- * 2^31 - 65537 tokens, key or value rows more than 2^27 bytes apart in uniprefill_attention, more
- * than 65535 sequences over the 4-bit cache.
+ * UP_ERR_UNSUPPORTED: sequences (max_kv_len) of more than 2^31 - 65537 tokens; in uniprefill_attention
+ * key or value rows more than 2^27 bytes apart, and more than 2^24 - 1 work-groups (per kv head one for every 128 rows,
+ * tokens times query heads per kv head, one for every sequence, and where long key ranges are cut one for every piece of
+ * their rows' tiles: 260111 sequences of one token with 64/64 heads are the most);
+ * over the 4-bit cache more than 65535 sequences, 2^22 - 1 query heads, or 2^31 - 1 times 64 cached tokens by max_kv_len.
  * None of these calls waits for the device or allocates; all can be captured into a graph (the host
  * arrays are read when the call is made).  A workspace is free again when the call's work has run: calls that may run at the same
  * time need one each. */

@@ -41,6 +41,7 @@ struct AttnArgs {
 // waves of a decode work-group, each on a kv head (D = 256: four, with twice the registers)
 constexpr UP_HD int q4_waves(int D) { return D == 256 ? 4 : 8; }
 constexpr int kQ4MaxWaveParts = 4;       // waves of a work-group that may share a kv head's keys
+constexpr int kQ4JoinWaves = 16;         // waves that join the pieces of a query head, at most
 // ... and waves per SIMD that its registers are held to
 constexpr UP_HD int q4_dense(int D) { return D == 64 ? 4 : D == 128 ? 2 : 1; }
 constexpr int kQ4Group = 64;        // elements that share one (lowest value, step) pair

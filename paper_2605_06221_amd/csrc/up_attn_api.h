@@ -59,6 +59,9 @@ int attn_geometry(const Problem& pb, const int32_t* cu, const int32_t* ck, AttnG
     return work * pb.Hkv / kCUs;
   };
   if (live * pb.Hkv < kCUs || (live * pb.Hkv < 2 * kCUs && 2.0 * (double)longest > 1.5 * keys_per_cu(128))) g->rows = 128;
+  // (work-items of a launch are counted in 32 bits: twice as many work-groups of 128 rows fit as of 256)
+  auto most_groups = [](int threads) { return (long long)UINT32_MAX / threads; };
+  if (((long long)pb.T * pb.Gq / 256 + pb.R) * pb.Hkv > most_groups(2 * 256)) g->rows = 128;
   const double fair = keys_per_cu(g->rows);
   g->parts = 1;
   g->slots = (long long)pb.T * pb.Gq / g->rows + pb.R;
@@ -92,7 +95,7 @@ int attn_geometry(const Problem& pb, const int32_t* cu, const int32_t* ck, AttnG
       g->total = off;
     }
   }
-  if (g->items * pb.Hkv > INT32_MAX || g->slots * pb.Hkv > INT32_MAX) return UP_ERR_UNSUPPORTED;
+  if (g->items * pb.Hkv > most_groups(2 * g->rows) || g->slots * pb.Hkv > most_groups(256)) return UP_ERR_UNSUPPORTED;
   return UP_OK;
 }
 
@@ -180,7 +183,8 @@ int q4_geometry(const Problem& pb, int max_len, bool mass, Q4Geometry* g) {
     off = align256(off + rows * (size_t)g->logit_stride * sizeof(float));
   }
   g->total = off;
-  if (pb.R > 65535 || layers > 65535 || steps > INT32_MAX || max_len > kMaxLength) return UP_ERR_UNSUPPORTED;
+  if (pb.R > 65535 || layers > 65535 || steps > INT32_MAX || max_len > kMaxLength || pb.Hq > UINT32_MAX / (64 * kQ4JoinWaves))
+    return UP_ERR_UNSUPPORTED;
   return UP_OK;
 }
 

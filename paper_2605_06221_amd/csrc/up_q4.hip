@@ -632,7 +632,6 @@ __global__ __launch_bounds__(64 * q4_waves(D), q4_dense(D)) void k_q4_attn(Q4Att
 
 // Joins the pieces of one query head of one sequence: the work-group's waves take the pieces in turn, eight in flight each, and
 // their sums are added in order.
-constexpr int kQ4JoinWaves = 16;
 template <int D>
 __global__ __launch_bounds__(64 * kQ4JoinWaves) void k_q4_join(Q4AttnArgs a) {
   constexpr int PER = D / 64, FLY = 8;

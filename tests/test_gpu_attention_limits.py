@@ -79,3 +79,23 @@ def test_values_leave_the_cache_rounded_once(dtype):
     up.uniprefill_cache_load_q4(p, _dev(rows), None, rows.shape[1], n, _dev(np.arange(n)), n, None, out, None, heads * D)
     torch.cuda.synchronize()
     assert torch.equal(out.double().cpu(), want)
+
+
+def test_attention_of_very_many_sequences():
+    """131072 sequences of one token, 64/64 heads: more work-groups of 512 threads than a launch can count.  A token that sees
+    its own key alone has its value, bit for bit, and its logit (a float sum of D products of bf16) as log-sum-exp."""
+    n, heads, D = 131072, 64, 64
+    _say("attention:", n, "sequences of one token")
+    q, k, v = (torch.randn(n, heads, D, dtype=BF, device="cuda") for _ in range(3))
+    out = torch.full((n + 1, heads, D), -7.0, dtype=BF, device="cuda")
+    lse = torch.full((heads, n), -7.0, device="cuda")
+    cu = np.arange(n + 1, dtype=np.int32)
+    p = up.make_params(num_seqs=n, total_tokens=n, block_size=64, num_q_heads=heads, num_kv_heads=heads, head_dim=D)
+    assert up.uniprefill_attention_plan(p, cu) == (up.UP_OK, 0)
+    up.uniprefill_attention(p, q, k, v, heads * D, _dev(cu), cu, None, None, None, 0, 1, out, heads * D, lse, n, None, 0)
+    torch.cuda.synchronize()
+    assert torch.equal(out[:n], v) and (out[n:] == -7.0).all()
+    for lo in range(0, n, 1 << 14):
+        a, b = q[lo:lo + (1 << 14)].double(), k[lo:lo + (1 << 14)].double()
+        x, size = (a * b).sum(2) / 8, (a * b).abs().sum(2) / 8
+        assert ((lse[:, lo:lo + (1 << 14)].double().T - x).abs() <= (D + 4) * F * size + 8 * F * (size + 1)).all()

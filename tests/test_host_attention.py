@@ -208,3 +208,17 @@ def test_evict_of_no_tokens_with_rows_beyond_what_is_counted():
     for pieces in ((1 << 31) - 1024, 1 << 32):
         assert _evict(max_len=0, row=16 * pieces, stride=16 * pieces, table=None, new=None, mass=None, kept=None,
                       mass_out=None) == up.UP_ERR_UNSUPPORTED
+
+
+def test_plans_refuse_what_a_launch_cannot_count():
+    # work-items of a launch are counted in 32 bits: 256 of them a work-group, one for each sequence and kv head and 128 tokens and kv head
+    for n, want in ((131072, up.UP_OK), (260111, up.UP_OK), (260112, up.UP_ERR_UNSUPPORTED)):
+        p = _params(num_seqs=n, total_tokens=n, num_q_heads=64, num_kv_heads=64, head_dim=64)
+        cu = np.arange(n + 1, dtype=np.int32)
+        assert up.uniprefill_attention_plan(p, cu, check=False)[0] == want
+        refused = dict(lse=None, ws=None, ws_bytes=0, out_stride=64 * 64, v_stride=64 * 64, cu_host=cu)
+        assert want == up.UP_OK or _attention(p, **refused) == want
+    # and 1024 for a query head of the launch that joins the pieces of a decode step
+    for heads, want in ((1 << 16) - 1, up.UP_OK), (1 << 16, up.UP_ERR_UNSUPPORTED):
+        p = _params(num_seqs=1, total_tokens=1, num_q_heads=64 * heads, num_kv_heads=heads, head_dim=64)
+        assert up.uniprefill_attention_q4_plan(p, 1000, False, check=False)[0] == want
