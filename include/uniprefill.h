@@ -594,7 +594,8 @@ int uniprefill_attention_q4(const up_params* p, const void* q, const void* k_cac
  *   (mass_out_stride >= budget, UP_ERR_SHAPE): entries j < new_len[r] are written;
  *   kept_idx is ascending.  mass must be finite.  kept_idx and mass_out overlap neither each other nor
  *   mass: a row of mass_out also holds the counts of a long sequence's choice while the call runs
- *   (the same address twice: UP_ERR_UNSUPPORTED).  Both block tables have rows of
+ *   (the same address twice: UP_ERR_UNSUPPORTED).  new_len [num_seqs] may be kv_len_dev itself (the lengths are
+ *   updated in place) and overlaps it in no other way (UP_ERR_UNSUPPORTED).  Both block tables have rows of
  *   kv_block_size-token pages that hold max_kv_len (block_table) and the smaller of
  *   budget and max_kv_len (new_table) tokens, else UP_ERR_SHAPE.  row_bytes, cache_row_stride:
  *   multiples of 16 (UP_ERR_ALIGN), row_bytes >= 16 and <= cache_row_stride.  More than 65535

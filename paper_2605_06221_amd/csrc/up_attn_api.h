@@ -363,6 +363,9 @@ int uniprefill_cache_evict(void* k_cache, void* v_cache, int64_t row_bytes, int6
   // (the kernels count 16-byte pieces in 31 bits, those of one row too where max_kv_len leaves no rows)
   if (num_seqs > 65535 || max_kv_len > kMaxLength || imax(most, 1) > (INT32_MAX - 1024) / (row_bytes / 16)) return UP_ERR_UNSUPPORTED;
   if (max_kv_len > 0 && ((const void*)mass == mass_out || (const void*)kept_idx == mass_out || (const void*)mass == kept_idx)) return UP_ERR_UNSUPPORTED;
+  // the lengths are read by the last launch too, which writes them: in place, or apart
+  const intptr_t apart = (intptr_t)new_len - (intptr_t)kv_len_dev, ends = (intptr_t)num_seqs * (intptr_t)sizeof(int32_t);
+  if (apart != 0 && apart > -ends && apart < ends) return UP_ERR_UNSUPPORTED;
   EvictArgs a{};
   a.k = (char*)k_cache; a.v = (char*)v_cache; a.row_bytes = row_bytes; a.cache_stride = cache_row_stride;
   a.mass = mass; a.mass_out = mass_out; a.mass_stride = mass_row_stride; a.mass_out_stride = mass_out_stride;

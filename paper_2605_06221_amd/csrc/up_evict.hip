@@ -266,7 +266,6 @@ __global__ __launch_bounds__(kEvictThreads) void k_evict_select(EvictArgs a) {
   const float* mass = a.mass + (long long)r * a.mass_stride;
   int32_t* kept = a.kept_idx + (long long)r * a.mass_out_stride;
   float* mass_out = a.mass_out + (long long)r * a.mass_out_stride;
-  if (tid == 0) a.new_len[r] = imin(len, a.budget);
   if (len <= a.budget) {
     for (int i = tid; i < len; i += kEvictThreads) {
       kept[i] = i;
@@ -306,13 +305,9 @@ __global__ __launch_bounds__(kSpreadThreads) void k_evict_spread(EvictArgs a) {
       for (int i = (int)blockIdx.x * kSpreadThreads + tid; i < kSpreadFound; i += (int)gridDim.x * kSpreadThreads) scratch[i] = 0;
     return;
   }
-  if (from >= len) {
-    if (WHAT == kWrite && from == 0 && tid == 0) a.new_len[r] = 0;
-    return;
-  }
+  if (from >= len) return;
   if (len <= a.budget) {
     if (WHAT == kWrite) {
-      if (from == 0 && tid == 0) a.new_len[r] = len;
       for (int i = from + tid; i < imin(len, from + kSpreadTokens); i += kSpreadThreads) kept[i] = i;
     }
     return;
@@ -411,16 +406,17 @@ __global__ __launch_bounds__(kSpreadThreads) void k_evict_spread(EvictArgs a) {
     out += __popcll(keeps);
     seen += __popcll(eq);
   }
-  if (from == 0 && tid == 0) a.new_len[r] = a.budget;
 }
 
-// The kept rows of a sequence as 16-byte pieces in a row, four of them of both caches per thread in flight.
+// The kept rows of a sequence as 16-byte pieces in a row, four of them of both caches per thread in flight, and how many rows they are.
 // MASS: the kept masses too.
 constexpr int kEvictPieces = 4;
 template <bool MASS>
 __global__ __launch_bounds__(256) void k_evict_move(EvictArgs a) {
   const int r = blockIdx.y;
   const int kept = imin(imin(imax(a.kv_len[r], 0), a.max_len), a.budget);
+  // (new_len may be kv_len: of the length before and the one that is kept the same number follows, so any order will do)
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.new_len[r] = kept;
   const unsigned pieces = (unsigned)(a.row_bytes / 16);
   const unsigned first = blockIdx.x * (256u * kEvictPieces) + threadIdx.x;
   long long src[kEvictPieces], dst[kEvictPieces];
@@ -475,15 +471,13 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
+  // (one work-group at least: it writes the lengths, also where no token can stay)
   const int most = a.budget < a.max_len ? a.budget : a.max_len;
-  if (most > 0) {
-    const long long pieces = (long long)most * (a.row_bytes / 16), each = 256 * kEvictPieces;
-    const dim3 grid((unsigned)((pieces + each - 1) / each), a.R);
-    if (spread) hipLaunchKernelGGL(k_evict_move<true>, grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(k_evict_move<false>, grid, dim3(256), 0, s, a);
-    e = hipGetLastError();
-  }
-  return e;
+  const long long pieces = (long long)most * (a.row_bytes / 16), each = 256 * kEvictPieces;
+  const dim3 grid(pieces > each ? (unsigned)((pieces + each - 1) / each) : 1u, a.R);
+  if (spread) hipLaunchKernelGGL(k_evict_move<true>, grid, dim3(256), 0, s, a);
+  else hipLaunchKernelGGL(k_evict_move<false>, grid, dim3(256), 0, s, a);
+  return hipGetLastError();
 }
 
 }  // namespace up

@@ -99,3 +99,37 @@ def test_attention_of_very_many_sequences():
         a, b = q[lo:lo + (1 << 14)].double(), k[lo:lo + (1 << 14)].double()
         x, size = (a * b).sum(2) / 8, (a * b).abs().sum(2) / 8
         assert ((lse[:, lo:lo + (1 << 14)].double().T - x).abs() <= (D + 4) * F * size + 8 * F * (size + 1)).all()
+
+
+@pytest.mark.parametrize("lengths,budget,max_len", [
+    ([5000, 10, 0, 300, 101, -3], 100, 5000), ([60000, 24577, 0, 9, 8999, 30000, 1 << 30], 9000, 60000), ([7, 0], 10, 0),
+])
+def test_eviction_updates_lengths_in_place(lengths, budget, max_len):
+    """new_len and kv_len_dev at one address: the choice, the rows and the lengths are those of a call with two."""
+    _say("eviction: lengths in place", lengths, budget)
+    rng = np.random.default_rng(budget)
+    R, page, row = len(lengths), 64, 32
+    most = min(budget, max_len)
+    per, new_per = -(-max_len // page) + 1, -(-most // page) + 1
+    table = np.arange(R * per, dtype=np.int32).reshape(R, per)
+    new_table = R * per + np.arange(R * new_per, dtype=np.int32).reshape(R, new_per)
+    before = _dev(rng.integers(0, 256, (R * (per + new_per) * page, row)).astype(np.uint8))
+    mass_host = rng.random((R, max_len + 1)).astype(np.float32)
+    mass, tables = _dev(mass_host), (_dev(table), _dev(new_table))
+    for _ in range(3):
+        found = []
+        for in_place in (False, True):
+            cache, lens = before.clone(), torch.tensor(lengths, dtype=torch.int32, device="cuda")
+            new_len = lens if in_place else torch.full_like(lens, -77)
+            kept_idx = torch.full((R, budget), -77, dtype=torch.int32, device="cuda")
+            mass_out = torch.full((R, budget), -7.0, device="cuda")
+            up.uniprefill_cache_evict(cache, None, row, row, mass, max_len + 1, lens, R, max_len, budget, 4, 6, tables[0], per, tables[1],
+                                      new_per, page, kept_idx, mass_out, budget, new_len)
+            torch.cuda.synchronize()
+            found.append((new_len, cache, kept_idx, mass_out))
+        assert found[1][0].tolist() == [min(max(n, 0), max_len, budget) for n in lengths]
+        for a, b in zip(*found):
+            assert torch.equal(a, b)
+    for r, n in enumerate(lengths):
+        stay = ao.evict_tokens(mass_host[r], min(max(n, 0), max_len), budget, 4, 6)
+        assert found[1][2][r, :len(stay)].tolist() == list(stay) and (found[1][2][r, len(stay):] == -77).all()

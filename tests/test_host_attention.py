@@ -222,3 +222,9 @@ def test_plans_refuse_what_a_launch_cannot_count():
     for heads, want in ((1 << 16) - 1, up.UP_OK), (1 << 16, up.UP_ERR_UNSUPPORTED):
         p = _params(num_seqs=1, total_tokens=1, num_q_heads=64 * heads, num_kv_heads=heads, head_dim=64)
         assert up.uniprefill_attention_q4_plan(p, 1000, False, check=False)[0] == want
+
+
+def test_evict_refuses_new_lengths_that_overlap_the_old_ones():
+    apart = dict(kept=A + 4096, mass_out=A + 8192, len=A + 12288, seqs=100)
+    for shift in (4, -4, 396, -396):
+        assert _evict(**dict(apart, new_len=A + 12288 + shift)) == up.UP_ERR_UNSUPPORTED
