@@ -141,7 +141,7 @@ int check_cu_k(const up_params* p, const int32_t* cu_host, const int32_t* cu_k_h
   if (cu_k_host == nullptr) return UP_ERR_NULL;
   if (cu_k_host[0] != 0) return UP_ERR_SHAPE;
   for (int r = 0; r < p->num_seqs; ++r)
-    if (cu_k_host[r + 1] - cu_k_host[r] < cu_host[r + 1] - cu_host[r]) return UP_ERR_SHAPE;
+    if ((int64_t)cu_k_host[r + 1] - cu_k_host[r] < (int64_t)cu_host[r + 1] - cu_host[r]) return UP_ERR_SHAPE;
   return UP_OK;
 }
 

@@ -228,3 +228,11 @@ def test_evict_refuses_new_lengths_that_overlap_the_old_ones():
     apart = dict(kept=A + 4096, mass_out=A + 8192, len=A + 12288, seqs=100)
     for shift in (4, -4, 396, -396):
         assert _evict(**dict(apart, new_len=A + 12288 + shift)) == up.UP_ERR_UNSUPPORTED
+
+
+def test_key_offsets_that_fall_out_of_range_are_refused():
+    # the difference of the last two leaves 32 bits
+    ck = np.array([0, 200000, -(1 << 31)], np.int32)
+    ratio = np.ones(2, np.float32)
+    assert up.uniprefill_attention_plan(_params(), CU, ck, check=False)[0] == up.UP_ERR_SHAPE
+    assert up.uniprefill_plan_chunked(_params(), CU, ck, ratio, check=False)[0] == up.UP_ERR_SHAPE
