@@ -31,7 +31,8 @@
  *                          size < 1; drop layers not strictly ascending
  *       UP_ERR_UNSUPPORTED head_dim not in {64,128,256}, or 256 with UP_F32
  *                          operands; num_q_heads % num_kv_heads != 0; more than
- *                          64 query heads per kv head; unknown dtype
+ *                          64 query heads per kv head; unknown dtype; rows more
+ *                          than 2^60 elements apart
  *       UP_ERR_ALIGN       a base pointer is not 16-byte aligned or a row stride
  *                          in bytes is not a multiple of 16
  *       UP_ERR_WORKSPACE   workspace is NULL or smaller than uniprefill_plan says

@@ -71,6 +71,9 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 
 int elem_bytes(int dt) { return dt == UP_BF16 ? 2 : 4; }
 
+// elements between rows up to which a stride in bytes stays within 64 bits
+constexpr int64_t kMostStride = (int64_t)1 << 60;
+
 // head rows of 512 bytes (fp32 operands, or 256 bf16 elements) only fit the 8-wave work-group
 bool narrow_only(const Problem& pb) { return pb.qk_is_f32 || pb.head_dim > 128; }
 
@@ -97,6 +100,7 @@ int check_params(const up_params* p, bool need_qk, bool need_hidden, Problem* pb
     if (p->q_row_stride < (int64_t)p->num_q_heads * p->head_dim ||
         p->k_row_stride < (int64_t)p->num_kv_heads * p->head_dim)
       return UP_ERR_SHAPE;
+    if (p->q_row_stride > kMostStride || p->k_row_stride > kMostStride) return UP_ERR_UNSUPPORTED;
     const int eb = elem_bytes(p->qk_dtype);
     if ((p->q_row_stride * eb) % 16 != 0 || (p->k_row_stride * eb) % 16 != 0) return UP_ERR_ALIGN;
     q.Gq = p->num_q_heads / p->num_kv_heads;
@@ -108,6 +112,7 @@ int check_params(const up_params* p, bool need_qk, bool need_hidden, Problem* pb
     if (p->hidden_dim < 1) return UP_ERR_SHAPE;
     if (p->hidden_dtype != UP_BF16 && p->hidden_dtype != UP_F32) return UP_ERR_UNSUPPORTED;
     if (p->hidden_row_stride < p->hidden_dim) return UP_ERR_SHAPE;
+    if (p->hidden_row_stride > kMostStride) return UP_ERR_UNSUPPORTED;
     q.hidden_elem_bytes = elem_bytes(p->hidden_dtype);
     if (((int64_t)p->hidden_dim * q.hidden_elem_bytes) % 16 != 0 ||
         (p->hidden_row_stride * q.hidden_elem_bytes) % 16 != 0)

@@ -102,6 +102,7 @@ int attn_geometry(const Problem& pb, const int32_t* cu, const int32_t* ck, AttnG
 // strides of a second tensor with head rows (values, outputs), in elements
 int check_row_stride(int64_t stride, int heads, int head_dim, int elem) {
   if (stride < (int64_t)heads * head_dim) return UP_ERR_SHAPE;
+  if (stride > kMostStride) return UP_ERR_UNSUPPORTED;
   if ((stride * elem) % 16 != 0) return UP_ERR_ALIGN;
   return UP_OK;
 }

@@ -236,3 +236,18 @@ def test_key_offsets_that_fall_out_of_range_are_refused():
     ratio = np.ones(2, np.float32)
     assert up.uniprefill_attention_plan(_params(), CU, ck, check=False)[0] == up.UP_ERR_SHAPE
     assert up.uniprefill_plan_chunked(_params(), CU, ck, ratio, check=False)[0] == up.UP_ERR_SHAPE
+
+
+@pytest.mark.parametrize("stride", [(1 << 60) + 16, 1 << 61, 1 << 62])
+def test_strides_whose_bytes_leave_64_bits_are_refused(stride):
+    f32 = dict(qk_dtype=up.UP_F32)
+    for given in (dict(q_row_stride=stride), dict(k_row_stride=stride)):
+        assert _attention(_params(**given, **f32)) == up.UP_ERR_UNSUPPORTED
+        assert up.uniprefill_attention_plan(_params(**given, **f32), CU, check=False)[0] == up.UP_ERR_UNSUPPORTED
+    assert _attention(_params(**f32), v_stride=stride) == up.UP_ERR_UNSUPPORTED
+    assert _attention(_params(**f32), out_stride=stride) == up.UP_ERR_UNSUPPORTED
+    assert _decode(out_stride=stride) == up.UP_ERR_UNSUPPORTED
+    for load in (False, True):
+        assert _store(load=load, v_stride=stride) == up.UP_ERR_UNSUPPORTED
+    p = _params(hidden_dim=64, hidden_row_stride=stride, hidden_dtype=up.UP_F32)
+    assert up.uniprefill_compact(p, A, None, A, 10, A, None, stream=0, check=False) == up.UP_ERR_UNSUPPORTED
