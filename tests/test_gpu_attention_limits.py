@@ -133,3 +133,40 @@ def test_eviction_updates_lengths_in_place(lengths, budget, max_len):
     for r, n in enumerate(lengths):
         stay = ao.evict_tokens(mass_host[r], min(max(n, 0), max_len), budget, 4, 6)
         assert found[1][2][r, :len(stay)].tolist() == list(stay) and (found[1][2][r, len(stay):] == -77).all()
+
+
+@pytest.mark.parametrize("lengths,budget,n_sink,n_recent,page", [
+    ([5, 0, 64, 65, 1000], 64, 4, 4, 16), ([3000, 10, 20000], 300, 128, 128, 7), ([60000, 24577, 0, 30000], 9000, 4, 100, 64),
+])
+def test_eviction_of_one_cache_alone(lengths, budget, n_sink, n_recent, page):
+    """v_cache NULL: the keys' rows, indices, masses and lengths as the oracle has them, from a call that nothing came before."""
+    _say("eviction of the keys alone", lengths, budget)
+    rng = np.random.default_rng(budget + 1)
+    R, most, row, stride = len(lengths), max(lengths), 48, 64
+    kept = [min(n, budget) for n in lengths]
+    old, new = [-(-n // page) for n in lengths], [-(-n // page) for n in kept]
+    pages, at = rng.permutation(sum(old) + sum(new)), 0
+    table, new_table = np.full((R, max(old)), -1, np.int32), np.full((R, max(new)), -1, np.int32)
+    for t, need in ((table, old), (new_table, new)):
+        for r, n in enumerate(need):
+            t[r, :n] = pages[at:at + n]
+            at += n
+    before = rng.integers(0, 256, (at * page, stride)).astype(np.uint8)
+    mass = rng.integers(0, 200, (R, most)).astype(np.float32)      # ties too
+    cache = _dev(before)
+    kept_idx, mass_out = torch.full((R, budget), -77, dtype=torch.int32, device="cuda"), torch.full((R, budget), -7.0, device="cuda")
+    new_len = torch.full((R,), -77, dtype=torch.int32, device="cuda")
+    up.uniprefill_cache_evict(cache, None, row, stride, _dev(mass), most, _dev(np.array(lengths, np.int32)), R, most, budget, n_sink,
+                              n_recent, _dev(table), table.shape[1], _dev(new_table), new_table.shape[1], page, kept_idx, mass_out, budget,
+                              new_len)
+    torch.cuda.synchronize()
+    want = before.copy()
+    for r, n in enumerate(lengths):
+        stay = ao.evict_tokens(mass[r], n, budget, n_sink, n_recent)
+        m = len(stay)
+        np.testing.assert_array_equal(kept_idx[r, :m].cpu().numpy(), stay)
+        np.testing.assert_array_equal(mass_out[r, :m].cpu().numpy(), mass[r][stay])
+        assert (kept_idx[r, m:] == -77).all() and (mass_out[r, m:] == -7.0).all()
+        want[ao.page_rows(new_table[r], m, page), :row] = before[ao.page_rows(table[r], n, page)[stay], :row]
+    assert new_len.tolist() == kept
+    np.testing.assert_array_equal(cache.cpu().numpy(), want)
