@@ -143,8 +143,10 @@ def ptr(x):
 def _stream(stream):
     if stream is None:
         import torch
-        # torch.cuda.current_stream().cuda_stream without the Stream object: 0.3 instead of 2.7 us of a call's 8
-        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+        # torch.cuda.current_stream().cuda_stream without the Stream object: 0.3 instead of 2.7 us of a call's 8.  The function is not
+        # part of torch's public interface: where a release lacks it, the public way.
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device()))
     if isinstance(stream, int):
         return ctypes.c_void_p(stream)
     return ctypes.c_void_p(stream.cuda_stream)

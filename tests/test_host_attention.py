@@ -251,3 +251,16 @@ def test_strides_whose_bytes_leave_64_bits_are_refused(stride):
         assert _store(load=load, v_stride=stride) == up.UP_ERR_UNSUPPORTED
     p = _params(hidden_dim=64, hidden_row_stride=stride, hidden_dtype=up.UP_F32)
     assert up.uniprefill_compact(p, A, None, A, 10, A, None, stream=0, check=False) == up.UP_ERR_UNSUPPORTED
+
+
+def test_the_current_stream_is_found_without_torchs_private_function(monkeypatch):
+    import types
+
+    import torch
+    from paper_2605_06221_amd import binding
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: types.SimpleNamespace(cuda_stream=4096))
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 8192 + device, raising=False)
+    assert binding._stream(None).value == 8195
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream")
+    assert binding._stream(None).value == 4096
