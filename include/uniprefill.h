@@ -487,7 +487,8 @@ int uniprefill_fused_top_p_chunked(const up_params* p, const void* q, const void
  * their rows' tiles: 260111 sequences of one token with 64/64 heads are the most);
  * over the 4-bit cache more than 65535 sequences, 2^22 - 1 query heads, or 2^31 - 1 times 64 cached tokens by max_kv_len.
  * None of these calls waits for the device or allocates; all can be captured into a graph (the host
- * arrays are read when the call is made).  A workspace is free again when the call's work has run: calls that may run at the same
+ * arrays are read when the call is made: a captured uniprefill_attention keeps its lengths, while
+ * uniprefill_attention_q4 and uniprefill_cache_evict read theirs on the device).  A workspace is free again when the call's work has run: calls that may run at the same
  * time need one each. */
 
 /* Causal attention of a packed batch (Eq. 2; "Sparsity Propagation": the layer
@@ -567,7 +568,11 @@ int uniprefill_cache_load_q4(const up_params* p, const void* k_cache, const void
  *                     in place); other entries are left as they are.
  *                     mass_row_stride >= max_kv_len (UP_ERR_SHAPE)
  *   workspace         from uniprefill_attention_q4_plan (want_mass: whether
- *                     mass_out will be given), 256-byte aligned
+ *                     mass_out will be given), 256-byte aligned.  With masses it
+ *                     holds a float per sequence, query head and token up to
+ *                     max_kv_len, however short the sequences are (64 sequences,
+ *                     32 heads, 131072 tokens: 1.07 GB)
+ * The cache is read once per 16 query heads of a kv head.
  * The codes enter the products as whole numbers and the steps in float; the
  * weights times their steps are rounded to bf16 for the product with the values. */
 int uniprefill_attention_q4_plan(const up_params* p, int32_t max_kv_len, int32_t want_mass,
@@ -595,7 +600,9 @@ int uniprefill_attention_q4(const up_params* p, const void* q, const void* k_cac
  *   (mass_out_stride >= budget, UP_ERR_SHAPE): entries j < new_len[r] are written;
  *   kept_idx is ascending.  mass must be finite.  kept_idx and mass_out overlap neither each other nor
  *   mass: a row of mass_out also holds the counts of a long sequence's choice while the call runs
- *   (the same address twice: UP_ERR_UNSUPPORTED).  new_len [num_seqs] may be kv_len_dev itself (the lengths are
+ *   (the same address twice: UP_ERR_UNSUPPORTED).  With max_kv_len >= 24576 many work-groups share a sequence's choice if the row has
+ *   room for their counts, budget >= 6152 + 2 * ceil(max_kv_len / 4096); under a smaller budget one
+ *   work-group takes each sequence, and longer (131072 tokens to 4096: 111 us, to 16384: 57).  new_len [num_seqs] may be kv_len_dev itself (the lengths are
  *   updated in place) and overlaps it in no other way (UP_ERR_UNSUPPORTED).  Both block tables have rows of
  *   kv_block_size-token pages that hold max_kv_len (block_table) and the smaller of
  *   budget and max_kv_len (new_table) tokens, else UP_ERR_SHAPE.  row_bytes, cache_row_stride:

@@ -15,6 +15,7 @@ constexpr int kMaxLength = INT32_MAX - 65536;
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // ---- attention of a packed batch
+// The geometry follows from the host's lengths: a captured call keeps those it was made with.
 // A work-group takes 256 rows (tokens x query heads of one kv head; 8 waves) of one sequence and walks over the
 // keys they see; 128 rows (4 waves) where work-groups of 256 would be fewer than the CUs, or fewer than twice as many with the
 // longest well beyond a CU's share (one prompt of 2048, 32/8 heads, 67 -> 57 us, float 500 -> 296; 2048 tokens after 6000 others
@@ -59,7 +60,8 @@ int attn_geometry(const Problem& pb, const int32_t* cu, const int32_t* ck, AttnG
     return work * pb.Hkv / kCUs;
   };
   if (live * pb.Hkv < kCUs || (live * pb.Hkv < 2 * kCUs && 2.0 * (double)longest > 1.5 * keys_per_cu(128))) g->rows = 128;
-  // (work-items of a launch are counted in 32 bits: twice as many work-groups of 128 rows fit as of 256)
+  // (work-items of a launch are counted in 32 bits, and one of more runs short without an error; twice as many work-groups
+  // of 128 rows fit as of 256)
   auto most_groups = [](int threads) { return (long long)UINT32_MAX / threads; };
   if (((long long)pb.T * pb.Gq / 256 + pb.R) * pb.Hkv > most_groups(2 * 256)) g->rows = 128;
   const double fair = keys_per_cu(g->rows);

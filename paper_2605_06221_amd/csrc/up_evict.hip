@@ -13,7 +13,9 @@ namespace up {
 namespace {
 
 constexpr int kEvictThreads = 1024, kEvictWaves = kEvictThreads / 64, kEvictFly = 8;
-// A longest sequence from which on many work-groups choose, where the budget leaves them room to count: their six launches cost what one
+// A longest sequence (by max_kv_len: the lengths are on the device) from which on many work-groups choose, where the budget leaves them room
+// to count in a row of mass_out, kSpreadCounts + 2 words a work-group, 6152 + 2 * max_kv_len / 4096; below that one work-group has to
+// (131072 tokens: 57 us to 16384, 111 to 4096, 101 to 1024).  Their six launches cost what one
 // work-group takes for 24576 tokens (with the move and reading back 8000 rows: 16384 tokens 37 against 43 us, 24576 43.4 and 43.6, 32768
 // 49.5 against 43.7, 131072 136 against 59, 200000 171 against 45).
 constexpr int kEvictLong = 24576;
