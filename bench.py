@@ -25,7 +25,8 @@ HBM_PEAK_GBS = 8000.0          # MI355X HBM3E
 MFMA_BF16_PEAK_TFLOPS = 2500.0  # dense bf16
 
 # sources in csrc/ that the sparsification path does not run
-OTHER_SOURCES = ("up_pipes_bench.hip", "up_attn.h", "up_attn.hip", "up_attn_api.h", "up_q4.hip", "up_evict.hip")
+OTHER_SOURCES = ("up_pipes_bench.hip", "up_attn.h", "up_attn.hip", "up_attn_api.h", "up_q4.hip", "up_evict.hip",
+                 "up_layers.h", "up_layers_api.h", "up_linear.hip", "up_pages.hip", "up_rotate.hip")
 
 TRAFFIC_FILE = os.path.join(ROOT, "profiles", "hbm_traffic.json")
 
@@ -34,7 +35,7 @@ def csrc_digest():
     """SHA-256 over the code of the sparsification path's kernel sources: what a counter measurement is valid
     for.  Comments and white space are left out (an edit to a comment does not change what was measured), and
     so are the stand-alone pipe microbenchmark, which is not part of the library, and the sources of the
-    attention layer's operators, whose kernels the measured calls do not launch."""
+    operators of the layers around a drop, whose kernels the measured calls do not launch."""
     import hashlib
     import re
     d = os.path.join(ROOT, "paper_2605_06221_amd", "csrc")

@@ -616,6 +616,142 @@ int uniprefill_cache_evict(void* k_cache, void* v_cache, int64_t row_bytes, int6
                            int32_t* kept_idx, float* mass_out, int64_t mass_out_stride, int32_t* new_len,
                            void* stream);
 
+/* ---- The layers between two drops --------------------------------------------
+ *
+ * A hybrid model's other layers run on the retained tokens too (Eq. 7): windowed
+ * attention, linear attention, what stands in front of an attention layer (the norm
+ * and the rotation of its heads, by the retained tokens' position ids), and the pages
+ * of the cache in the model's own type.  Rows, strides, paged addressing, streams,
+ * errors and ownership as above; none of these calls waits for the device or
+ * allocates, and all can be captured into a graph.  A workspace is free again when the
+ * call's work has run: calls that may run at the same time need one each.  In the two
+ * kinds of attention it is the order of a sequence's tokens that counts: after a drop,
+ * windows and decays count retained tokens. */
+
+/* uniprefill_attention in which the token at position p = P_r + i sees, of keys 0 .. p,
+ * only the last `window` ones (itself among them) and the first n_sink:
+ *     i <= p and (i > p - window or i < n_sink).
+ * window >= 1 and n_sink >= 0, else UP_ERR_RANGE; a window of at least the longest
+ * sequence's keys is uniprefill_attention.  All else, the log-sum-exp over the visible
+ * keys among it, is as there: other arguments, layouts of the keys, precision and
+ * refusals.  Keys that no token sees are not read: entries of the table that name only
+ * such keys may name no page.  The workspace is that of
+ * uniprefill_attention_window_plan with the same lengths, window and n_sink. */
+int uniprefill_attention_window_plan(const up_params* p, const int32_t* cu_seqlens_host,
+                                     const int32_t* cu_seqlens_k_host, int32_t window, int32_t n_sink,
+                                     size_t* workspace_bytes);
+int uniprefill_attention_window(const up_params* p, const void* q, const void* k, const void* v, int64_t v_row_stride,
+                                const int32_t* cu_seqlens_dev, const int32_t* cu_seqlens_host,
+                                const int32_t* cu_seqlens_k_dev, const int32_t* cu_seqlens_k_host,
+                                const int32_t* block_table, int64_t block_table_stride, int32_t kv_block_size,
+                                int32_t window, int32_t n_sink, void* out, int64_t out_row_stride, float* lse_out,
+                                int64_t lse_row_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The same for one new token per sequence over a paged cache, lengths on the device:
+ * query row r (total_tokens == num_seqs, else UP_ERR_SHAPE) stands at the end of the
+ * first kv_len_dev[r] tokens of its block-table row (values outside [0, max_kv_len]
+ * count as the nearer end; a sequence of length 0 gets zeros and lse -inf).
+ * max_kv_len sizes the launch and the workspace; a block-table row must hold it
+ * (UP_ERR_SHAPE).  A captured call follows the lengths from replay to replay. */
+int uniprefill_attention_window_step_plan(const up_params* p, int32_t max_kv_len, int32_t window, int32_t n_sink,
+                                          size_t* workspace_bytes);
+int uniprefill_attention_window_step(const up_params* p, const void* q, const void* k_cache, const void* v_cache,
+                                     int64_t v_row_stride, const int32_t* kv_len_dev, int32_t max_kv_len,
+                                     const int32_t* block_table, int64_t block_table_stride, int32_t kv_block_size,
+                                     int32_t window, int32_t n_sink, void* out, int64_t out_row_stride, float* lse_out,
+                                     int64_t lse_row_stride, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Linear attention with a decay for each kv head: a sequence carries, for every kv
+ * head h, a state S [head_dim, head_dim] in float (row: element of the key, column:
+ * element of the value), and its tokens one after the other
+ *     S <- lam_h S + k_t^T v_t,      out[t, h'] = softmax_scale * q[t, h'] S
+ * for the query heads h' of kv head h, with lam_h = exp(log_decay[h]) (device float
+ * [num_kv_heads]; values above 0 count as 0).  softmax_scale as everywhere: 0 is
+ * 1/sqrt(head_dim).
+ *   states       device float, num_states slots of [num_kv_heads, head_dim, head_dim],
+ *                state_stride elements between slots (a multiple of 4, at least the slot;
+ *                UP_ERR_ALIGN / UP_ERR_SHAPE)
+ *   state_in     int32 [num_seqs] on the device: the slot that a sequence's state starts
+ *                from; outside [0, num_states), or state_in NULL: from zero
+ *   state_out    the slot that it is stored to after the sequence's tokens (without
+ *                tokens: as it started); outside [0, num_states), or NULL: not stored
+ *   A sequence may start from the slot it stores to.  A slot that one sequence stores to
+ *   must be named by no other sequence of the call.
+ * States are float throughout: bf16 products are exact, the decayed keys and values keep
+ * 24 bits.  In the outputs the decayed logits and the state are taken in 16 bits.
+ *   out          as for uniprefill_attention; overlaps none of q, k, v
+ *   workspace    from uniprefill_linear_attention_plan with the same lengths
+ *                (256-byte aligned; 0 bytes, and NULL, where no sequence is cut)
+ * Refusals as for uniprefill_attention; more than (2^32 - 1) / 256 work-groups of 32
+ * state columns: UP_ERR_UNSUPPORTED. */
+int uniprefill_linear_attention_plan(const up_params* p, const int32_t* cu_seqlens_host, size_t* workspace_bytes);
+int uniprefill_linear_attention(const up_params* p, const void* q, const void* k, const void* v, int64_t v_row_stride,
+                                const int32_t* cu_seqlens_dev, const int32_t* cu_seqlens_host, const float* log_decay,
+                                float* states, int64_t state_stride, int64_t num_states, const int32_t* state_in,
+                                const int32_t* state_out, void* out, int64_t out_row_stride, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
+/* The same for one token per sequence (total_tokens == num_seqs, else UP_ERR_SHAPE),
+ * token r of sequence r: float throughout, no workspace.  A sequence whose state_in and
+ * state_out lie outside the pool (an unused place of the batch) leaves every state
+ * as it is. */
+int uniprefill_linear_attention_step(const up_params* p, const void* q, const void* k, const void* v, int64_t v_row_stride,
+                                     const float* log_decay, float* states, int64_t state_stride, int64_t num_states,
+                                     const int32_t* state_in, const int32_t* state_out, void* out, int64_t out_row_stride,
+                                     void* stream);
+
+/* Norm and rotation of the heads in front of an attention layer, in one pass.  Every
+ * head row x of q and k becomes
+ *     y = x / sqrt(mean(x_i^2) + eps) * weight      (eps > 0; eps == 0: y = x)
+ * and of y the first rot_dim elements are turned, pair by pair, by the token's position:
+ *     (a, b) -> (a cos - b sin, b cos + a sin),  angle = pos[t] * inv_freq[j],
+ * pair j being elements (j, j + rot_dim / 2), or (2j, 2j + 1) where pairs is not 0.
+ * Values v are copied bit by bit.  Computed in float (angles in double: they are good
+ * at any position) and rounded once.
+ *   q, k, v            rows t < total_tokens (and t < count_dev[0] when that device pointer is
+ *                      given); a tensor and its output may both be NULL
+ *   q_weight, k_weight [head_dim] in qk_dtype, 16-byte aligned; NULL: 1
+ *   eps                0, or a normal float above 0 (UP_ERR_RANGE); 0 with a weight: UP_ERR_RANGE
+ *   pos                int32 [T]; inv_freq float [rot_dim / 2], both on the device
+ *   rot_dim            0 (nothing turns; pos, inv_freq may be NULL) to head_dim (UP_ERR_RANGE), a
+ *                      multiple of 16 (UP_ERR_UNSUPPORTED)
+ *   q_out              row t in place t; may be q itself (same stride).  Otherwise outputs overlap no input
+ *   k_out, v_out       row t in place slots[t] (int64, as uniprefill_slot_mapping and
+ *                      uniprefill_append_pages write them; rows whose slot lies outside
+ *                      [0, num_slots) are left out, no slot may be named twice), or with slots NULL in place t
+ *                      (k_out may then be k itself)
+ * Squares of a row must stay within float. */
+int uniprefill_norm_rotate(const up_params* p, const void* q, const void* k, const void* v, int64_t v_row_stride,
+                           const void* q_weight, const void* k_weight, float eps, const int32_t* pos,
+                           const float* inv_freq, int32_t rot_dim, int32_t pairs, const int32_t* count_dev,
+                           void* q_out, int64_t q_out_row_stride, void* k_out, int64_t k_out_row_stride, void* v_out,
+                           int64_t v_out_row_stride, const int64_t* slots, int64_t num_slots, void* stream);
+
+/* Pages for a step's new tokens: sequence r has kv_len_dev[r] tokens in the pages of its
+ * block-table row and receives num_new_dev[r] more (negative values count as 0).  The
+ * pages that it lacks are taken from the end of the free list, free_pages[num_free_dev[0]
+ * - 1] first, sequence by sequence, and entered into its row.  The first sequence that
+ * cannot be served -- too few free pages, more pages than block_table_stride, more new
+ * tokens in all than `capacity`, a length beyond 2^31 - 1 -- and all after it receive
+ * nothing.  All arrays on the device:
+ *   new_len_dev      [num_seqs] lengths afterwards; may be kv_len_dev itself (and overlaps it in no
+ *                    other way: UP_ERR_UNSUPPORTED)
+ *   free_left_dev    [1] free pages left; may be num_free_dev itself
+ *   cu_seqlens_dev   [num_seqs + 1] offsets of the tokens served (what the calls above take as
+ *                    cu_seqlens), cu_seqlens_k_dev those of the keys (new_len_dev added up; sums beyond
+ *                    2^31 - 1 are written as that)
+ *   pos, slots       [capacity] int32 position and int64 slot of every token served, in order; the rest
+ *                    is filled with 0 and -1, the slot that the cache's entry points leave out
+ *   num_served_dev   [1] sequences served
+ * Lengths beyond what a row of the table holds are not served; entries of the table up to a sequence's
+ * length must name its pages.  capacity and num_seqs up to 2^31 - 65537 (UP_ERR_UNSUPPORTED),
+ * kv_block_size >= 1 and block_table_stride >= 0 (UP_ERR_RANGE). */
+int uniprefill_append_pages(const int32_t* kv_len_dev, const int32_t* num_new_dev, int32_t num_seqs,
+                            int32_t kv_block_size, int32_t* block_table, int64_t block_table_stride,
+                            const int32_t* free_pages, const int32_t* num_free_dev, int32_t* free_left_dev,
+                            int32_t* new_len_dev, int32_t* cu_seqlens_dev, int32_t* cu_seqlens_k_dev, int32_t* pos,
+                            int64_t* slots, int64_t capacity, int32_t* num_served_dev, void* stream);
+
 /* Static, never NULL. */
 const char* uniprefill_status_string(int status);
 

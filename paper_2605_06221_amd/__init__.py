@@ -10,6 +10,9 @@ from .binding import (  # noqa: F401
     uniprefill_fused_top_p_lse, uniprefill_score_partial, uniprefill_scores_from_partials, uniprefill_plan_chunked, uniprefill_score_chunked, uniprefill_select_chunked, uniprefill_fused_chunked,
     uniprefill_attention_plan, uniprefill_attention, uniprefill_q4_row_bytes, uniprefill_cache_store_q4,
     uniprefill_cache_load_q4, uniprefill_attention_q4_plan, uniprefill_attention_q4, uniprefill_cache_evict,
+    uniprefill_attention_window_plan, uniprefill_attention_window, uniprefill_attention_window_step_plan,
+    uniprefill_attention_window_step, uniprefill_linear_attention_plan, uniprefill_linear_attention, uniprefill_linear_attention_step,
+    uniprefill_norm_rotate, uniprefill_append_pages,
     UP_PHASE_PLAN, UP_PHASE_ROW_STATS, UP_PHASE_MERGE_STATS, UP_PHASE_SWEEP_SELECT, UP_PHASE_GATHER,
     UP_PHASE_ALL, UP_PHASE_GATHER_IN_SELECT,
 )

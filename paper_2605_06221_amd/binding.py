@@ -30,7 +30,10 @@ EXPORTS = ["uniprefill_plan", "uniprefill_score", "uniprefill_select", "uniprefi
            "uniprefill_scores_from_partials", "uniprefill_fused_static",
            "uniprefill_attention_plan", "uniprefill_attention", "uniprefill_q4_row_bytes", "uniprefill_cache_store_q4",
            "uniprefill_cache_load_q4", "uniprefill_attention_q4_plan", "uniprefill_attention_q4",
-           "uniprefill_cache_evict", "uniprefill_status_string"]
+           "uniprefill_cache_evict", "uniprefill_attention_window_plan", "uniprefill_attention_window",
+           "uniprefill_attention_window_step_plan", "uniprefill_attention_window_step", "uniprefill_linear_attention_plan",
+           "uniprefill_linear_attention", "uniprefill_linear_attention_step", "uniprefill_norm_rotate", "uniprefill_append_pages",
+           "uniprefill_status_string"]
 
 UP_PHASE_PLAN, UP_PHASE_ROW_STATS, UP_PHASE_MERGE_STATS, UP_PHASE_SWEEP_SELECT, UP_PHASE_GATHER = 1, 2, 4, 8, 16
 UP_PHASE_ALL = 31
@@ -109,6 +112,18 @@ def _load():
     lib.uniprefill_attention_q4.argtypes = [P, vp, vp, vp, i64, i32p, i32] + table + [vp, i64, f32p, i64, f32p, f32p, i64] + ws + [vp]
     lib.uniprefill_cache_evict.argtypes = [vp, vp, i64, i64, f32p, i64, i32p, i32, i32, i32, i32, i32, i32p, i64, i32p, i64, i32,
                                            i32p, f32p, i64, i32p, vp]
+    band, f32 = [i32, i32], ctypes.c_float          # window, n_sink
+    lib.uniprefill_attention_window_plan.argtypes = [P, i32p, i32p] + band + [ctypes.POINTER(sz)]
+    lib.uniprefill_attention_window.argtypes = [P, vp, vp, vp, i64, i32p, i32p] + keys + table + band + [vp, i64, f32p, i64] + ws + [vp]
+    lib.uniprefill_attention_window_step_plan.argtypes = [P, i32] + band + [ctypes.POINTER(sz)]
+    lib.uniprefill_attention_window_step.argtypes = [P, vp, vp, vp, i64, i32p, i32] + table + band + [vp, i64, f32p, i64] + ws + [vp]
+    states = [f32p, f32p, i64, i64, i32p, i32p]     # log_decay, states, state_stride, num_states, state_in, state_out
+    lib.uniprefill_linear_attention_plan.argtypes = [P, i32p, ctypes.POINTER(sz)]
+    lib.uniprefill_linear_attention.argtypes = [P, vp, vp, vp, i64, i32p, i32p] + states + [vp, i64] + ws + [vp]
+    lib.uniprefill_linear_attention_step.argtypes = [P, vp, vp, vp, i64] + states + [vp, i64, vp]
+    lib.uniprefill_norm_rotate.argtypes = [P, vp, vp, vp, i64, vp, vp, f32, i32p, f32p, i32, i32, i32p, vp, i64, vp, i64, vp, i64, vp, i64,
+                                           vp]
+    lib.uniprefill_append_pages.argtypes = [i32p, i32p, i32, i32, i32p, i64, i32p, i32p, i32p, i32p, i32p, i32p, i32p, vp, i64, i32p, vp]
     for name in EXPORTS[:-1]:
         getattr(lib, name).restype = ctypes.c_int
     lib.uniprefill_q4_row_bytes.restype = i64
@@ -512,3 +527,86 @@ def uniprefill_cache_evict(k_cache, v_cache, row_bytes, cache_row_stride, mass, 
                                      int(new_table_stride), int(kv_block_size), ptr(kept_idx), ptr(mass_out),
                                      int(mass_out_stride), ptr(new_len), _stream(stream))
     return _check(st, "uniprefill_cache_evict", check)
+
+
+def uniprefill_attention_window_plan(p: up_params, cu_seqlens_host: np.ndarray, cu_seqlens_k_host, window, n_sink, *, check: bool = True):
+    """Returns (status, workspace_bytes)."""
+    ws = ctypes.c_size_t(0)
+    st = _lib.uniprefill_attention_window_plan(ctypes.byref(p), ptr(cu_seqlens_host), ptr(cu_seqlens_k_host), int(window), int(n_sink),
+                                               ctypes.byref(ws))
+    _check(st, "uniprefill_attention_window_plan", check)
+    return st, int(ws.value)
+
+
+def uniprefill_attention_window(p, q, k, v, v_row_stride, cu_seqlens_dev, cu_seqlens_host, cu_seqlens_k_dev, cu_seqlens_k_host,
+                                block_table, block_table_stride, kv_block_size, window, n_sink, out, out_row_stride, lse_out,
+                                lse_row_stride, workspace, workspace_bytes, stream=None, check=True):
+    st = _lib.uniprefill_attention_window(ctypes.byref(p), ptr(q), ptr(k), ptr(v), int(v_row_stride), ptr(cu_seqlens_dev),
+                                          ptr(cu_seqlens_host), ptr(cu_seqlens_k_dev), ptr(cu_seqlens_k_host), ptr(block_table),
+                                          int(block_table_stride), int(kv_block_size), int(window), int(n_sink), ptr(out),
+                                          int(out_row_stride), ptr(lse_out), int(lse_row_stride), ptr(workspace), workspace_bytes,
+                                          _stream(stream))
+    return _check(st, "uniprefill_attention_window", check)
+
+
+def uniprefill_attention_window_step_plan(p: up_params, max_kv_len, window, n_sink, *, check: bool = True):
+    """Returns (status, workspace_bytes)."""
+    ws = ctypes.c_size_t(0)
+    st = _lib.uniprefill_attention_window_step_plan(ctypes.byref(p), int(max_kv_len), int(window), int(n_sink), ctypes.byref(ws))
+    _check(st, "uniprefill_attention_window_step_plan", check)
+    return st, int(ws.value)
+
+
+def uniprefill_attention_window_step(p, q, k_cache, v_cache, v_row_stride, kv_len_dev, max_kv_len, block_table, block_table_stride,
+                                     kv_block_size, window, n_sink, out, out_row_stride, lse_out, lse_row_stride, workspace,
+                                     workspace_bytes, stream=None, check=True):
+    st = _lib.uniprefill_attention_window_step(ctypes.byref(p), ptr(q), ptr(k_cache), ptr(v_cache), int(v_row_stride),
+                                               ptr(kv_len_dev), int(max_kv_len), ptr(block_table), int(block_table_stride),
+                                               int(kv_block_size), int(window), int(n_sink), ptr(out), int(out_row_stride),
+                                               ptr(lse_out), int(lse_row_stride), ptr(workspace), workspace_bytes, _stream(stream))
+    return _check(st, "uniprefill_attention_window_step", check)
+
+
+def uniprefill_linear_attention_plan(p: up_params, cu_seqlens_host: np.ndarray, *, check: bool = True):
+    """Returns (status, workspace_bytes)."""
+    ws = ctypes.c_size_t(0)
+    st = _lib.uniprefill_linear_attention_plan(ctypes.byref(p), ptr(cu_seqlens_host), ctypes.byref(ws))
+    _check(st, "uniprefill_linear_attention_plan", check)
+    return st, int(ws.value)
+
+
+def uniprefill_linear_attention(p, q, k, v, v_row_stride, cu_seqlens_dev, cu_seqlens_host, log_decay, states, state_stride, num_states,
+                                state_in, state_out, out, out_row_stride, workspace, workspace_bytes, stream=None, check=True):
+    st = _lib.uniprefill_linear_attention(ctypes.byref(p), ptr(q), ptr(k), ptr(v), int(v_row_stride), ptr(cu_seqlens_dev),
+                                          ptr(cu_seqlens_host), ptr(log_decay), ptr(states), int(state_stride), int(num_states),
+                                          ptr(state_in), ptr(state_out), ptr(out), int(out_row_stride), ptr(workspace),
+                                          workspace_bytes, _stream(stream))
+    return _check(st, "uniprefill_linear_attention", check)
+
+
+def uniprefill_linear_attention_step(p, q, k, v, v_row_stride, log_decay, states, state_stride, num_states, state_in, state_out, out,
+                                     out_row_stride, stream=None, check=True):
+    st = _lib.uniprefill_linear_attention_step(ctypes.byref(p), ptr(q), ptr(k), ptr(v), int(v_row_stride), ptr(log_decay), ptr(states),
+                                               int(state_stride), int(num_states), ptr(state_in), ptr(state_out), ptr(out),
+                                               int(out_row_stride), _stream(stream))
+    return _check(st, "uniprefill_linear_attention_step", check)
+
+
+def uniprefill_norm_rotate(p, q, k, v, v_row_stride, q_weight, k_weight, eps, pos, inv_freq, rot_dim, pairs, count_dev, q_out,
+                           q_out_row_stride, k_out, k_out_row_stride, v_out, v_out_row_stride, slots, num_slots, stream=None,
+                           check=True):
+    st = _lib.uniprefill_norm_rotate(ctypes.byref(p), ptr(q), ptr(k), ptr(v), int(v_row_stride), ptr(q_weight), ptr(k_weight),
+                                     float(eps), ptr(pos), ptr(inv_freq), int(rot_dim), int(pairs), ptr(count_dev), ptr(q_out),
+                                     int(q_out_row_stride), ptr(k_out), int(k_out_row_stride), ptr(v_out), int(v_out_row_stride),
+                                     ptr(slots), int(num_slots), _stream(stream))
+    return _check(st, "uniprefill_norm_rotate", check)
+
+
+def uniprefill_append_pages(kv_len_dev, num_new_dev, num_seqs, kv_block_size, block_table, block_table_stride, free_pages,
+                            num_free_dev, free_left_dev, new_len_dev, cu_seqlens_dev, cu_seqlens_k_dev, pos, slots, capacity,
+                            num_served_dev, stream=None, check=True):
+    st = _lib.uniprefill_append_pages(ptr(kv_len_dev), ptr(num_new_dev), int(num_seqs), int(kv_block_size), ptr(block_table),
+                                      int(block_table_stride), ptr(free_pages), ptr(num_free_dev), ptr(free_left_dev),
+                                      ptr(new_len_dev), ptr(cu_seqlens_dev), ptr(cu_seqlens_k_dev), ptr(pos), ptr(slots),
+                                      int(capacity), ptr(num_served_dev), _stream(stream))
+    return _check(st, "uniprefill_append_pages", check)

@@ -11,6 +11,9 @@ namespace up {
 // pieces of part_keys keys that `keys` keys are cut into (both below 2^31: their sum leaves an int, not 32 bits)
 UP_HD int attn_pieces(int keys, int part_keys) { return (int)(((unsigned)keys + (unsigned)part_keys - 1u) / (unsigned)part_keys); }
 
+// keys that a work-group of `rows` rows stages at a time, head rows of row_bytes bytes
+constexpr UP_HD int attn_stage_keys(int row_bytes, int rows) { return (row_bytes == 512 ? 32 : 64) * (rows == 256 ? 2 : 1); }
+
 struct AttnArgs {
   const char* q;
   const char* k;
@@ -35,6 +38,12 @@ struct AttnArgs {
   int32_t* base;                   // [slots] first piece of a row tile that is cut, -1 for one that is not
   float* o_part;                   // [pieces][Hkv][rows][D] sums of weighted values
   float* ml_part;                  // [pieces][Hkv][rows] pairs (reference in log2 units, sum of weights)
+  // windowed attention; window == 0: every token sees all keys before it
+  int window, n_sink;              // token at position p sees keys p - window + 1 .. p and 0 .. n_sink - 1
+  int sinks;                       // n_sink in whole stages
+  int reach;                       // keys that a row tile walks over at most
+  const int32_t* kv_len;           // one new token per sequence: its length, on the device; else nullptr
+  int max_len;
 };
 
 // --- the 4-bit KV cache

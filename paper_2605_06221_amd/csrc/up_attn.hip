@@ -52,6 +52,7 @@ struct AttnTile {
   static constexpr int SUB = KT / 32;
   static constexpr int TILES = WAVES == 8 ? 2 : 1;        // tiles staged at a time
   static constexpr int KS = KT * TILES;
+  static_assert(KS == attn_stage_keys(SRCB, ROWS), "what the host counts with");
   static constexpr int PIECES = KS * PPR / THREADS;       // pieces per thread and staging
   static constexpr int ROWSTEP = THREADS / PPR;
   static constexpr int KREG = SRCB / 32;                  // 16-byte registers of a lane's half row
@@ -123,11 +124,35 @@ struct AttnItem {
   long long piece;      // number of the piece in the workspace, -1: the tile is not cut
 };
 
+// Windowed attention (WINDOW): the keys that a row tile sees are the sinks and a band.  The tile walks over them on an axis of its
+// own: `sinks` places for the first keys (a whole number of stages; 0 where the band begins among them), then the band from key `low` on
+// (a multiple of 8, so that the rows of a load stay within a page).
+struct AttnBand {
+  int sinks, low;
+};
+__device__ __forceinline__ AttnBand attn_band(const AttnArgs& a, int pos0) {
+  const int first = pos0 - a.window + 1;                        // first key in the first row's window
+  return first <= a.sinks ? AttnBand{0, 0} : AttnBand{a.sinks, first & ~7};
+}
+// keys (places) that a sequence's tiles walk over at most
+template <bool WINDOW>
+__device__ __forceinline__ int attn_reach(const AttnArgs& a, int Lk) { return WINDOW ? imin(Lk, a.reach) : Lk; }
+
+// Length of sequence r where the lengths are on the device (one new token each)
+__device__ __forceinline__ int attn_step_keys(const AttnArgs& a, int r) { return imax(0, imin(a.kv_len[r], a.max_len)); }
+
 // Work item -> sequence, row tile, piece.  Unsplit launches number the row tiles without a prefix sum
 // (a few numbers stand for nothing); split launches walk over the sequences' counts, 256 at a time.
-template <int WAVES, bool SPLIT>
+template <int WAVES, bool SPLIT, bool WINDOW>
 __device__ __forceinline__ bool attn_locate(const AttnArgs& a, int item, AttnItem& w, long long* sm) {
   constexpr int THREADS = 64 * WAVES, ROWS = 32 * WAVES;
+  if (WINDOW && a.kv_len != nullptr) {      // one new token each: a.parts pieces of every sequence
+    w.r = item / a.parts;
+    w.part = item % a.parts;
+    w.tile = 0;
+    w.piece = SPLIT ? item : -1;
+    return true;
+  }
   if (!SPLIT) {
     w.r = attn_slot_sequence(a, item);
     w.tile = item - (int)attn_slot_base(a, w.r);
@@ -146,7 +171,7 @@ __device__ __forceinline__ bool attn_locate(const AttnArgs& a, int item, AttnIte
     if (r < a.R) {
       const long long N = a.cu[r + 1] - a.cu[r];
       const long long tiles = (N * a.Gq + ROWS - 1) / ROWS;
-      parts = attn_pieces(a.cu_k[r + 1] - a.cu_k[r], a.part_keys);
+      parts = attn_pieces(attn_reach<WINDOW>(a, a.cu_k[r + 1] - a.cu_k[r]), a.part_keys);
       ni = tiles * parts;
       np = parts > 1 ? ni : 0;
     }
@@ -185,7 +210,7 @@ __device__ __forceinline__ bool attn_locate(const AttnArgs& a, int item, AttnIte
   return false;
 }
 
-template <bool F32, int D, int WAVES, bool PAGED, bool SPLIT>
+template <bool F32, int D, int WAVES, bool PAGED, bool SPLIT, bool WINDOW>
 __global__ __launch_bounds__(64 * WAVES, (AttnTile<F32, D, WAVES>::DENSE)) void k_attn(AttnArgs a) {
   typedef AttnTile<F32, D, WAVES> T;
   // (two variables per buffer, not one array of buffers: the compiler then knows that a load into one and reads of
@@ -198,19 +223,32 @@ __global__ __launch_bounds__(64 * WAVES, (AttnTile<F32, D, WAVES>::DENSE)) void 
   // the last row tiles, which see the most keys, start first
   const int kvh = blockIdx.x % a.Hkv;
   AttnItem w;
-  if (!attn_locate<WAVES, SPLIT>(a, a.items - 1 - (int)(blockIdx.x / a.Hkv), w, scan)) return;
-  const int c0 = a.cu[w.r], N = a.cu[w.r + 1] - c0;
-  const int ck0 = a.cu_k[w.r], Lk = a.cu_k[w.r + 1] - ck0;
+  if (!attn_locate<WAVES, SPLIT, WINDOW>(a, a.items - 1 - (int)(blockIdx.x / a.Hkv), w, scan)) return;
+  const bool step = WINDOW && a.kv_len != nullptr;
+  const int c0 = step ? w.r : a.cu[w.r], N = step ? 1 : a.cu[w.r + 1] - c0;
+  const int ck0 = step ? 0 : a.cu_k[w.r], Lk = step ? attn_step_keys(a, w.r) : a.cu_k[w.r + 1] - ck0;
+  if (step && Lk == 0) {      // nothing is seen: zeros, and the logarithm of nothing
+    if (w.part != 0) return;
+    if (SPLIT && kvh == 0 && tid == 0) a.base[w.r] = -1;
+    char* dst = a.out + (long long)w.r * a.out_stride_b + (long long)kvh * a.Gq * T::SRCB;
+    for (int i = tid; i < a.Gq * T::PPR; i += T::THREADS) ((u32x4*)dst)[i] = u32x4{0, 0, 0, 0};
+    if (a.lse != nullptr && tid < a.Gq) a.lse[(long long)(kvh * a.Gq + tid) * a.lse_stride + w.r] = -INFINITY;
+    return;
+  }
   const long long row0 = (long long)w.tile * T::ROWS;
   const long long rows_left = (long long)N * a.Gq - row0;
   const int nrow = rows_left < T::ROWS ? (int)rows_left : T::ROWS;
   const int tok0 = (int)(row0 / a.Gq), rem0 = (int)(row0 % a.Gq);
   const int pos0 = Lk - N + tok0;                                  // position of the first row's token
-  const int visible = pos0 + (rem0 + nrow - 1) / a.Gq + 1;         // keys that the last row sees
+  const int last_pos = pos0 + (rem0 + nrow - 1) / a.Gq;
+  const AttnBand band = WINDOW ? attn_band(a, pos0) : AttnBand{0, 0};
+  const int visible = band.sinks + last_pos + 1 - band.low;        // keys that the last row sees (places of the tile's axis)
+  const int band_first = WINDOW ? imax(0, pos0 - a.window + 1) : 0;
+  auto key_at = [&](int place) { return WINDOW && place >= band.sinks ? place - band.sinks + band.low : place; };
   const int k_begin = SPLIT ? w.part * a.part_keys : 0;
   const int k_end = SPLIT && a.part_keys < visible - k_begin ? k_begin + a.part_keys : visible;
   if (SPLIT && kvh == 0 && w.part == 0 && tid == 0)
-    a.base[attn_slot_base(a, w.r) + w.tile] = w.piece < 0 ? -1 : (int)w.piece;
+    a.base[step ? w.r : attn_slot_base(a, w.r) + w.tile] = w.piece < 0 ? -1 : (int)w.piece;
   if (k_begin >= visible) return;
 
   // ---- this lane's row
@@ -220,6 +258,7 @@ __global__ __launch_bounds__(64 * WAVES, (AttnTile<F32, D, WAVES>::DENSE)) void 
   const int tok = (rem0 + x) / a.Gq, hh = (rem0 + x) % a.Gq;
   const int pos = pos0 + tok;
   const int wave_last = pos0 + (rem0 + imin(uwave * 32 + 31, nrow - 1)) / a.Gq;
+  const int wave_first = pos0 + (rem0 + imin(uwave * 32, nrow - 1)) / a.Gq;
   constexpr int HOFF = F32 ? T::SRCB / 2 : 16, KSTEP = F32 ? 16 : 32;
   u32x4 qf[T::KREG];
   {
@@ -268,7 +307,9 @@ __global__ __launch_bounds__(64 * WAVES, (AttnTile<F32, D, WAVES>::DENSE)) void 
 #pragma unroll
     for (int i = 0; i < T::PIECES; ++i) {
       const int r0 = i * T::ROWSTEP + uwave * WROWS;
-      const long long row = row_of(imin(k0 + r0 + lrow, Lk - 1));
+      int key = imin(k0 + r0 + lrow, Lk - 1);
+      if (WINDOW && key >= a.n_sink && key < band_first) key = band_first;      // (what no row sees is not read: its page may be gone)
+      const long long row = row_of(key);
       load_to_lds(k_head + row * a.k_stride_b + k_at[i & 1], sk + r0 * T::PPR);
       load_to_lds(v_head + row * a.v_stride_b + v_at, sv + r0 * T::PPR);
     }
@@ -310,8 +351,10 @@ __global__ __launch_bounds__(64 * WAVES, (AttnTile<F32, D, WAVES>::DENSE)) void 
 #pragma unroll
       for (int sub = 0; sub < T::SUB; ++sub)
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (k0 + sub * 32 + 8 * (e >> 2) + 4 * half + (e & 3) > pos) s[sub][e] = -INFINITY;
+        for (int e = 0; e < 16; ++e) {
+          const int key = k0 + sub * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
+          if (key > pos || (WINDOW && key <= pos - a.window && key >= a.n_sink)) s[sub][e] = -INFINITY;
+        }
     }
     float mx = s[0][0];
 #pragma unroll
@@ -417,12 +460,41 @@ __global__ __launch_bounds__(64 * WAVES, (AttnTile<F32, D, WAVES>::DENSE)) void 
   };
   auto last_tiles = [&](int k0, const u32x4* sk, const u32x4* sv) __attribute__((always_inline)) {
     if (!wave_live) return;
-    for (int u = 0; u < T::TILES; ++u)
-      if (k0 + u * T::KT <= wave_last && k0 + u * T::KT < k_end) tile(std::true_type{}, k0 + u * T::KT, sk + u * NEXT, sv + u * NEXT);
+    for (int u = 0; u < T::TILES; ++u) {
+      const int key = key_at(k0) + u * T::KT;
+      if (WINDOW && key >= a.n_sink && key + T::KT - 1 <= wave_first - a.window) continue;      // all before the wave's windows
+      if (key <= wave_last && k0 + u * T::KT < k_end) tile(std::true_type{}, key, sk + u * NEXT, sv + u * NEXT);
+    }
   };
-  stage_any(k_begin, sk0, sv0);
+  stage_any(key_at(k_begin), sk0, sv0);
   staged();
   int k0 = k_begin;
+  if constexpr (WINDOW) {
+    // Stages that every row sees whole lie in the middle of the band, or among the sinks.
+    auto whole = [&](int place) {
+      const int key = key_at(place);
+      return place + T::KS <= k_end && key + T::KS - 1 <= pos0 && (key > last_pos - a.window || key + T::KS <= a.n_sink);
+    };
+    auto stage = [&](int place, u32x4* sk, u32x4* sv) __attribute__((always_inline)) {
+      if (place >= k_end) return;
+      const int key = key_at(place);
+      if (in_runs && key + T::KS <= Lk && (key >= band_first || key + T::KS <= a.n_sink)) stage_run(key, sk, sv);
+      else stage_any(key, sk, sv);
+    };
+    auto tiles = [&](int place, const u32x4* sk, const u32x4* sv) __attribute__((always_inline)) {
+      if (whole(place)) whole_tiles(key_at(place), sk, sv);
+      else last_tiles(place, sk, sv);
+    };
+    for (; k0 < k_end; k0 += 2 * T::KS) {
+      stage(k0 + T::KS, sk1, sv1);
+      tiles(k0, sk0, sv0);
+      staged();
+      if (k0 + T::KS >= k_end) break;
+      stage(k0 + 2 * T::KS, sk0, sv0);
+      tiles(k0 + T::KS, sk1, sv1);
+      staged();
+    }
+  } else {
   const int whole = in_runs ? imin(imin(k_end, pos0 + 1), Lk - T::KS) - T::KS : k_begin - 1;
   for (; k0 + T::KS <= whole; k0 += 2 * T::KS) {
     stage_run(k0 + T::KS, sk1, sv1);
@@ -440,6 +512,7 @@ __global__ __launch_bounds__(64 * WAVES, (AttnTile<F32, D, WAVES>::DENSE)) void 
     if (k0 + 2 * T::KS < k_end) stage_any(k0 + 2 * T::KS, sk0, sv0);
     last_tiles(k0 + T::KS, sk1, sv1);
     staged();
+  }
   }
 
   l = half_sum(l);
@@ -474,19 +547,22 @@ __global__ __launch_bounds__(64 * WAVES, (AttnTile<F32, D, WAVES>::DENSE)) void 
 }
 
 // Joins the pieces of the row tiles that were cut: a wave per row, the pieces in order.
-template <bool F32, int D>
+template <bool F32, int D, bool WINDOW>
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int kvh = blockIdx.x % a.Hkv, slot = blockIdx.x / a.Hkv;
-  const int r = attn_slot_sequence(a, slot), c0 = a.cu[r], N = a.cu[r + 1] - c0, Lk = a.cu_k[r + 1] - a.cu_k[r];
-  const int tile = slot - (int)attn_slot_base(a, r);
+  const bool step = WINDOW && a.kv_len != nullptr;
+  const int r = step ? slot : attn_slot_sequence(a, slot), c0 = step ? r : a.cu[r], N = step ? 1 : a.cu[r + 1] - c0;
+  const int Lk = step ? attn_step_keys(a, r) : a.cu_k[r + 1] - a.cu_k[r];
+  const int tile = step ? 0 : slot - (int)attn_slot_base(a, r);
   const long long row0 = (long long)tile * a.rows, rows_left = (long long)N * a.Gq - row0;
   if (rows_left <= 0) return;
   const int first = a.base[slot];
   if (first < 0) return;
   const int nrow = rows_left < a.rows ? (int)rows_left : a.rows;
   const int tok0 = (int)(row0 / a.Gq), rem0 = (int)(row0 % a.Gq);
-  const int visible = Lk - N + tok0 + (rem0 + nrow - 1) / a.Gq + 1;
+  const AttnBand band = WINDOW ? attn_band(a, Lk - N + tok0) : AttnBand{0, 0};
+  const int visible = band.sinks + Lk - N + tok0 + (rem0 + nrow - 1) / a.Gq + 1 - band.low;
   const int parts = attn_pieces(visible, a.part_keys);      // pieces that saw a key
   constexpr int PER = D / 64;
   for (int x = blockIdx.y * 4 + wave; x < nrow; x += gridDim.y * 4) {
@@ -516,24 +592,29 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
   }
 }
 
-template <bool F32, int D, int WAVES, bool PAGED>
+template <bool F32, int D, int WAVES, bool PAGED, bool WINDOW>
 static hipError_t launch_attn(const AttnArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)a.items * a.Hkv), block(64 * WAVES);
   if (a.part_keys == 0) {
-    hipLaunchKernelGGL((k_attn<F32, D, WAVES, PAGED, false>), grid, block, 0, s, a);
+    hipLaunchKernelGGL((k_attn<F32, D, WAVES, PAGED, false, WINDOW>), grid, block, 0, s, a);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL((k_attn<F32, D, WAVES, PAGED, true>), grid, block, 0, s, a);
+  hipLaunchKernelGGL((k_attn<F32, D, WAVES, PAGED, true, WINDOW>), grid, block, 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((k_attn_join<F32, D>), dim3((unsigned)a.slots * a.Hkv, 8), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((k_attn_join<F32, D, WINDOW>), dim3((unsigned)a.slots * a.Hkv, 8), dim3(256), 0, s, a);
   return hipGetLastError();
+}
+
+template <bool F32, int D, bool PAGED>
+static hipError_t launch_attn_rows(const AttnArgs& a, hipStream_t s) {
+  if (a.window > 0) return a.rows == 256 ? launch_attn<F32, D, 8, PAGED, true>(a, s) : launch_attn<F32, D, 4, PAGED, true>(a, s);
+  return a.rows == 256 ? launch_attn<F32, D, 8, PAGED, false>(a, s) : launch_attn<F32, D, 4, PAGED, false>(a, s);
 }
 
 template <bool F32, int D>
 static hipError_t launch_attn_form(const AttnArgs& a, hipStream_t s) {
-  if (a.rows == 256) return a.block_table != nullptr ? launch_attn<F32, D, 8, true>(a, s) : launch_attn<F32, D, 8, false>(a, s);
-  return a.block_table != nullptr ? launch_attn<F32, D, 4, true>(a, s) : launch_attn<F32, D, 4, false>(a, s);
+  return a.block_table != nullptr ? launch_attn_rows<F32, D, true>(a, s) : launch_attn_rows<F32, D, false>(a, s);
 }
 
 hipError_t launch_attention(const AttnArgs& a, bool f32, int D, hipStream_t s) {

@@ -22,8 +22,13 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 // are even and stay: 244 us, 254 in work-groups of 128).  Where the rows alone leave
 // the chip idle all the same -- decode rows and short chunks on long caches -- the keys of every row tile are cut into
 // pieces of part_keys and the pieces joined.
+struct AttnWindow {
+  int window, n_sink;
+};
 struct AttnGeometry {
   int rows;
+  int sinks;                 // windowed attention: the sinks in whole stages
+  int reach;                 // ... and the keys that a row tile walks over at most
   int part_keys, parts;      // 0, 1: not cut
   long long items;           // work-groups per kv head
   long long pieces;          // row tiles x pieces of the sequences that are cut
@@ -39,7 +44,15 @@ struct AttnGeometry {
 // 1000 tokens, 32/8 heads, 28 -> 39 (not cut).  Pieces shorter than 512 keys (256 float) cost more to join than they save.
 double attn_key_us(bool f32, int D) { return f32 ? (D == 64 ? 0.06 : 0.13) : D == 64 ? 0.01 : D == 128 ? 0.015 : 0.04; }
 
-int attn_geometry(const Problem& pb, const int32_t* cu, const int32_t* ck, AttnGeometry* g) {
+// Keys that a tile of `rows` rows walks over at most: the sinks in whole stages, and the windows of its tokens, which begin up to 7 keys early.
+long long attn_window_reach(const Problem& pb, const AttnWindow& w, int rows, int* sinks) {
+  const long long unit = attn_stage_keys(pb.head_dim * (pb.qk_is_f32 ? 4 : 2), rows), whole = (w.n_sink + unit - 1) / unit * unit;
+  // (as many sinks as no sequence has tokens: the band begins among them everywhere)
+  *sinks = whole > kMaxLength ? kMaxLength : (int)whole;
+  return *sinks + (long long)w.window + rows / pb.Gq + 2 + 7;
+}
+
+int attn_geometry(const Problem& pb, const int32_t* cu, const int32_t* ck, AttnGeometry* g, const AttnWindow* w = nullptr) {
   const int D = pb.head_dim;
   *g = AttnGeometry{};
   g->rows = 256;
@@ -51,11 +64,14 @@ int attn_geometry(const Problem& pb, const int32_t* cu, const int32_t* ck, AttnG
   }
   if (longest > kMaxLength) return UP_ERR_UNSUPPORTED;
   auto tiles_of = [&](long long N, int rows) { return (N * pb.Gq + rows - 1) / rows; };
+  auto reach_of = [&](int rows) { return w != nullptr ? attn_window_reach(pb, *w, rows, &g->sinks) : (long long)INT32_MAX; };
+  longest = longest < reach_of(128) ? longest : reach_of(128);
   auto keys_per_cu = [&](int rows) {
     double work = 0;
     for (int r = 0; r < pb.R; ++r) {
       const long long N = cu[r + 1] - cu[r], L = ck[r + 1] - ck[r], tiles = tiles_of(N, rows);
-      if (N > 0) work += (double)tiles * (double)(L - N) + 0.5 * (double)(tiles + 1) * (double)N;
+      const double all = (double)tiles * (double)(L - N) + 0.5 * (double)(tiles + 1) * (double)N, most = (double)tiles * (double)reach_of(rows);
+      if (N > 0) work += all < most ? all : most;
     }
     return work * pb.Hkv / kCUs;
   };
@@ -65,6 +81,9 @@ int attn_geometry(const Problem& pb, const int32_t* cu, const int32_t* ck, AttnG
   auto most_groups = [](int threads) { return (long long)UINT32_MAX / threads; };
   if (((long long)pb.T * pb.Gq / 256 + pb.R) * pb.Hkv > most_groups(2 * 256)) g->rows = 128;
   const double fair = keys_per_cu(g->rows);
+  const long long reach = reach_of(g->rows);
+  g->reach = reach < INT32_MAX ? (int)reach : INT32_MAX;
+  auto pieces_of = [&](int r, long long part) { return attn_pieces(imin(ck[r + 1] - ck[r], g->reach), (int)part); };
   g->parts = 1;
   g->slots = (long long)pb.T * pb.Gq / g->rows + pb.R;
   g->items = g->slots;
@@ -74,7 +93,7 @@ int attn_geometry(const Problem& pb, const int32_t* cu, const int32_t* ck, AttnG
     const long long part = (want + 127) / 128 * 128;
     double rows = 0;      // rows of float sums that the pieces leave
     for (int r = 0; r < pb.R; ++r) {
-      const long long N = cu[r + 1] - cu[r], n = attn_pieces(ck[r + 1] - ck[r], (int)part);
+      const long long N = cu[r + 1] - cu[r], n = pieces_of(r, part);
       if (n > 1) rows += (double)(N * pb.Hq) * (double)n;
     }
     const double gain = ((double)longest - fair - (double)part) * attn_key_us(pb.qk_is_f32, D) * g->rows / 128, cost = 6.0 + rows * D * 8.0 / 3e6;
@@ -83,7 +102,7 @@ int attn_geometry(const Problem& pb, const int32_t* cu, const int32_t* ck, AttnG
       g->parts = attn_pieces((int)longest, (int)part);
       g->items = 0;
       for (int r = 0; r < pb.R; ++r) {
-        const long long tiles = tiles_of(cu[r + 1] - cu[r], g->rows), n = attn_pieces(ck[r + 1] - ck[r], (int)part);
+        const long long tiles = tiles_of(cu[r + 1] - cu[r], g->rows), n = pieces_of(r, part);
         g->items += tiles * n;
         if (n > 1) g->pieces += tiles * n;
       }
@@ -101,6 +120,33 @@ int attn_geometry(const Problem& pb, const int32_t* cu, const int32_t* ck, AttnG
   return UP_OK;
 }
 
+// One new token per sequence, lengths on the device: the keys that it can see at most are cut into pieces for about two work-groups per CU.
+int attn_step_geometry(const Problem& pb, int max_len, const AttnWindow& w, AttnGeometry* g) {
+  *g = AttnGeometry{};
+  if (max_len > kMaxLength) return UP_ERR_UNSUPPORTED;
+  g->rows = 128;
+  const long long reach = attn_window_reach(pb, w, g->rows, &g->sinks);
+  g->reach = (int)(reach < max_len ? reach : max_len);
+  const long long groups = (long long)pb.R * pb.Hkv, want = groups > 0 ? (2 * kCUs + groups - 1) / groups : 1;
+  long long part = ((g->reach + want - 1) / want + 127) / 128 * 128;
+  if (part < 512) part = 512;
+  g->parts = imax(1, attn_pieces(g->reach, (int)part));
+  g->slots = pb.R;
+  g->items = (long long)pb.R * g->parts;
+  if (g->parts > 1) {
+    g->part_keys = (int)part;
+    g->pieces = g->items;
+    size_t off = align256((size_t)g->slots * sizeof(int32_t));
+    g->o_off = off;
+    off = align256(off + (size_t)g->pieces * pb.Hkv * g->rows * pb.head_dim * sizeof(float));
+    g->ml_off = off;
+    off = align256(off + (size_t)g->pieces * pb.Hkv * g->rows * 2 * sizeof(float));
+    g->total = off;
+  }
+  if (g->items * pb.Hkv > (long long)UINT32_MAX / 512) return UP_ERR_UNSUPPORTED;
+  return UP_OK;
+}
+
 // strides of a second tensor with head rows (values, outputs), in elements
 int check_row_stride(int64_t stride, int heads, int head_dim, int elem) {
   if (stride < (int64_t)heads * head_dim) return UP_ERR_SHAPE;
@@ -110,6 +156,75 @@ int check_row_stride(int64_t stride, int heads, int head_dim, int elem) {
 }
 
 bool aligned_to(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1u)) == 0; }
+
+void attn_band_args(const AttnGeometry& g, const AttnWindow* w, AttnArgs* a) {
+  if (w == nullptr) return;
+  a->window = w->window; a->n_sink = w->n_sink; a->sinks = g.sinks; a->reach = g.reach;
+}
+void attn_piece_args(const AttnGeometry& g, void* workspace, AttnArgs* a) {
+  if (g.part_keys == 0) return;
+  a->base = (int32_t*)((char*)workspace + g.base_off);
+  a->o_part = (float*)((char*)workspace + g.o_off);
+  a->ml_part = (float*)((char*)workspace + g.ml_off);
+}
+
+int attention_plan_impl(const up_params* p, const int32_t* cu_seqlens_host, const int32_t* cu_seqlens_k_host, const AttnWindow* w,
+                        size_t* workspace_bytes) {
+  Problem pb;
+  int st = check_params(p, true, false, &pb);
+  if (st != UP_OK) return st;
+  if (workspace_bytes == nullptr) return UP_ERR_NULL;
+  if ((st = check_cu(p, cu_seqlens_host)) != UP_OK) return st;
+  if (cu_seqlens_k_host != nullptr && (st = check_cu_k(p, cu_seqlens_host, cu_seqlens_k_host)) != UP_OK) return st;
+  AttnGeometry g;
+  if ((st = attn_geometry(pb, cu_seqlens_host, cu_seqlens_k_host != nullptr ? cu_seqlens_k_host : cu_seqlens_host, &g,
+                          w)) != UP_OK)
+    return st;
+  *workspace_bytes = g.total;
+  return UP_OK;
+}
+
+int attention_impl(const up_params* p, const void* q, const void* k, const void* v, int64_t v_row_stride,
+                   const int32_t* cu_seqlens_dev, const int32_t* cu_seqlens_host, const int32_t* cu_seqlens_k_dev,
+                   const int32_t* cu_seqlens_k_host, const PagedKeys& paged, const AttnWindow* w, void* out, int64_t out_row_stride,
+                   float* lse_out, int64_t lse_row_stride, void* workspace, size_t workspace_bytes, void* stream) {
+  KeySide ks;
+  int st = optional_key_side(cu_seqlens_k_dev, cu_seqlens_k_host, &paged, &ks);
+  if (st != UP_OK) return st;
+  Problem pb;
+  if ((st = check_params(p, true, false, &pb)) != UP_OK) return st;
+  if (!cu_seqlens_dev || (pb.T > 0 && (!q || !k || !v || !out))) return UP_ERR_NULL;
+  if ((st = check_cu(p, cu_seqlens_host)) != UP_OK) return st;
+  if ((st = check_key_side(p, cu_seqlens_host, ks)) != UP_OK) return st;
+  const int e = pb.qk_is_f32 ? 4 : 2;
+  if ((st = check_row_stride(v_row_stride, pb.Hkv, pb.head_dim, e)) != UP_OK) return st;
+  if ((st = check_row_stride(out_row_stride, pb.Hq, pb.head_dim, e)) != UP_OK) return st;
+  if (lse_out != nullptr && lse_row_stride < pb.T) return UP_ERR_SHAPE;
+  if (pb.k_stride * e > kMaxRowStride || v_row_stride * e > kMaxRowStride) return UP_ERR_UNSUPPORTED;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return UP_ERR_ALIGN;
+  if (!aligned_to(lse_out, 4) || !aligned_to(paged.block_table, 4)) return UP_ERR_ALIGN;
+  const int32_t* ck = ks.ctx ? cu_seqlens_k_host : cu_seqlens_host;
+  AttnGeometry g;
+  if ((st = attn_geometry(pb, cu_seqlens_host, ck, &g, w)) != UP_OK) return st;
+  if (g.total > 0 && (workspace == nullptr || workspace_bytes < g.total)) return UP_ERR_WORKSPACE;
+  if (g.total > 0 && !aligned_to(workspace, 256)) return UP_ERR_ALIGN;
+  if (pb.T == 0) return UP_OK;
+  AttnArgs a{};
+  a.q = (const char*)q; a.k = (const char*)k; a.v = (const char*)v; a.out = (char*)out; a.lse = lse_out;
+  a.cu = cu_seqlens_dev; a.cu_k = ks.ctx ? cu_seqlens_k_dev : cu_seqlens_dev;
+  if (ks.paged != nullptr) {
+    a.block_table = paged.block_table; a.table_stride = paged.table_stride; a.kv_block = paged.kv_block;
+    a.kv_magic = 0xFFFFFFFFu / (unsigned)paged.kv_block;
+  }
+  a.q_stride_b = pb.q_stride * e; a.k_stride_b = pb.k_stride * e; a.v_stride_b = v_row_stride * e;
+  a.out_stride_b = out_row_stride * e; a.lse_stride = lse_row_stride;
+  a.c = pb.scale * 1.44269504088896340736f;
+  a.R = pb.R; a.Hq = pb.Hq; a.Hkv = pb.Hkv; a.Gq = pb.Gq;
+  a.rows = g.rows; a.slots = (int)g.slots; a.items = (int)g.items; a.part_keys = g.part_keys; a.parts = g.parts;
+  attn_band_args(g, w, &a);
+  attn_piece_args(g, workspace, &a);
+  return launch_attention(a, pb.qk_is_f32, pb.head_dim, (hipStream_t)stream) == hipSuccess ? UP_OK : UP_ERR_HIP;
+}
 
 // ---- the 4-bit cache
 int check_q4_cache(const Problem& pb, const void* k_cache, const void* v_cache, int64_t cache_row_stride) {
@@ -205,17 +320,7 @@ extern "C" {
 
 int uniprefill_attention_plan(const up_params* p, const int32_t* cu_seqlens_host, const int32_t* cu_seqlens_k_host,
                               size_t* workspace_bytes) {
-  Problem pb;
-  int st = check_params(p, true, false, &pb);
-  if (st != UP_OK) return st;
-  if (workspace_bytes == nullptr) return UP_ERR_NULL;
-  if ((st = check_cu(p, cu_seqlens_host)) != UP_OK) return st;
-  if (cu_seqlens_k_host != nullptr && (st = check_cu_k(p, cu_seqlens_host, cu_seqlens_k_host)) != UP_OK) return st;
-  AttnGeometry g;
-  if ((st = attn_geometry(pb, cu_seqlens_host, cu_seqlens_k_host != nullptr ? cu_seqlens_k_host : cu_seqlens_host, &g)) != UP_OK)
-    return st;
-  *workspace_bytes = g.total;
-  return UP_OK;
+  return attention_plan_impl(p, cu_seqlens_host, cu_seqlens_k_host, nullptr, workspace_bytes);
 }
 
 int uniprefill_attention(const up_params* p, const void* q, const void* k, const void* v, int64_t v_row_stride,
@@ -224,46 +329,9 @@ int uniprefill_attention(const up_params* p, const void* q, const void* k, const
                          const int32_t* block_table, int64_t block_table_stride, int32_t kv_block_size, void* out,
                          int64_t out_row_stride, float* lse_out, int64_t lse_row_stride, void* workspace,
                          size_t workspace_bytes, void* stream) {
-  const PagedKeys paged{block_table, block_table_stride, kv_block_size};
-  KeySide ks;
-  int st = optional_key_side(cu_seqlens_k_dev, cu_seqlens_k_host, &paged, &ks);
-  if (st != UP_OK) return st;
-  Problem pb;
-  if ((st = check_params(p, true, false, &pb)) != UP_OK) return st;
-  if (!cu_seqlens_dev || (pb.T > 0 && (!q || !k || !v || !out))) return UP_ERR_NULL;
-  if ((st = check_cu(p, cu_seqlens_host)) != UP_OK) return st;
-  if ((st = check_key_side(p, cu_seqlens_host, ks)) != UP_OK) return st;
-  const int e = pb.qk_is_f32 ? 4 : 2;
-  if ((st = check_row_stride(v_row_stride, pb.Hkv, pb.head_dim, e)) != UP_OK) return st;
-  if ((st = check_row_stride(out_row_stride, pb.Hq, pb.head_dim, e)) != UP_OK) return st;
-  if (lse_out != nullptr && lse_row_stride < pb.T) return UP_ERR_SHAPE;
-  if (pb.k_stride * e > kMaxRowStride || v_row_stride * e > kMaxRowStride) return UP_ERR_UNSUPPORTED;
-  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return UP_ERR_ALIGN;
-  if (!aligned_to(lse_out, 4) || !aligned_to(block_table, 4)) return UP_ERR_ALIGN;
-  const int32_t* ck = ks.ctx ? cu_seqlens_k_host : cu_seqlens_host;
-  AttnGeometry g;
-  if ((st = attn_geometry(pb, cu_seqlens_host, ck, &g)) != UP_OK) return st;
-  if (g.total > 0 && (workspace == nullptr || workspace_bytes < g.total)) return UP_ERR_WORKSPACE;
-  if (g.total > 0 && !aligned_to(workspace, 256)) return UP_ERR_ALIGN;
-  if (pb.T == 0) return UP_OK;
-  AttnArgs a{};
-  a.q = (const char*)q; a.k = (const char*)k; a.v = (const char*)v; a.out = (char*)out; a.lse = lse_out;
-  a.cu = cu_seqlens_dev; a.cu_k = ks.ctx ? cu_seqlens_k_dev : cu_seqlens_dev;
-  if (ks.paged != nullptr) {
-    a.block_table = block_table; a.table_stride = block_table_stride; a.kv_block = kv_block_size;
-    a.kv_magic = 0xFFFFFFFFu / (unsigned)kv_block_size;
-  }
-  a.q_stride_b = pb.q_stride * e; a.k_stride_b = pb.k_stride * e; a.v_stride_b = v_row_stride * e;
-  a.out_stride_b = out_row_stride * e; a.lse_stride = lse_row_stride;
-  a.c = pb.scale * 1.44269504088896340736f;
-  a.R = pb.R; a.Hq = pb.Hq; a.Hkv = pb.Hkv; a.Gq = pb.Gq;
-  a.rows = g.rows; a.slots = (int)g.slots; a.items = (int)g.items; a.part_keys = g.part_keys; a.parts = g.parts;
-  if (g.part_keys > 0) {
-    a.base = (int32_t*)((char*)workspace + g.base_off);
-    a.o_part = (float*)((char*)workspace + g.o_off);
-    a.ml_part = (float*)((char*)workspace + g.ml_off);
-  }
-  return launch_attention(a, pb.qk_is_f32, pb.head_dim, (hipStream_t)stream) == hipSuccess ? UP_OK : UP_ERR_HIP;
+  return attention_impl(p, q, k, v, v_row_stride, cu_seqlens_dev, cu_seqlens_host, cu_seqlens_k_dev, cu_seqlens_k_host,
+                        PagedKeys{block_table, block_table_stride, kv_block_size}, nullptr, out, out_row_stride, lse_out, lse_row_stride,
+                        workspace, workspace_bytes, stream);
 }
 
 int64_t uniprefill_q4_row_bytes(int32_t num_kv_heads, int32_t head_dim) {
@@ -381,3 +449,5 @@ int uniprefill_cache_evict(void* k_cache, void* v_cache, int64_t row_bytes, int6
 }
 
 }  // extern "C"
+
+#include "up_layers_api.h"
