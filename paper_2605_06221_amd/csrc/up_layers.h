@@ -22,6 +22,9 @@ struct LinearArgs {
   long long q_stride_b, k_stride_b, v_stride_b, out_stride_b;
   float scale;
   int R, Hq, Hkv, Gq;
+  int piece;                       // tokens of a piece (a multiple of 32); longer sequences are cut
+  int slots;                       // pieces of all sequences (an upper bound)
+  float* adds;                     // [2 T / piece + 1][Hkv][D][D] what the pieces of cut sequences add to the state; nullptr: none is cut
 };
 
 // --- norm and rotation
@@ -62,11 +65,13 @@ struct PagesArgs {
 };
 
 #if defined(__HIPCC__)
+hipError_t launch_linear(const LinearArgs& a, bool f32, int D, hipStream_t s);
 hipError_t launch_linear_tokens(const LinearArgs& a, bool f32, int D, hipStream_t s);
 hipError_t launch_rotate(const RotateArgs& a, bool f32, hipStream_t s);
 hipError_t launch_pages(const PagesArgs& a, hipStream_t s);
 #else
 // the host-only build of the argument checks has no kernels to launch
+inline hipError_t launch_linear(const LinearArgs&, bool, int, hipStream_t) { return hipSuccess; }
 inline hipError_t launch_linear_tokens(const LinearArgs&, bool, int, hipStream_t) { return hipSuccess; }
 inline hipError_t launch_rotate(const RotateArgs&, bool, hipStream_t) { return hipSuccess; }
 inline hipError_t launch_pages(const PagesArgs&, hipStream_t) { return hipSuccess; }

@@ -45,6 +45,28 @@ int linear_args(const up_params* p, const void* q, const void* k, const void* v,
   return UP_OK;
 }
 
+// Sequences are cut into pieces of so many tokens that the batch makes about two work-groups for every CU (as many as its registers
+// hold), none shorter than 256.
+struct LinearGeometry {
+  int piece;
+  long long slots;
+  size_t total;
+};
+int linear_geometry(const Problem& pb, const int32_t* cu, LinearGeometry* g) {
+  long long piece = ((long long)pb.T * pb.Hkv / (2 * kCUs) + 63) / 64 * 64;
+  if (piece < 256) piece = 256;
+  g->piece = (int)piece;
+  g->slots = pb.T / piece + pb.R;
+  g->total = 0;
+  for (int r = 0; r < pb.R; ++r)
+    if (cu[r + 1] - cu[r] > piece) g->total = (size_t)(2ll * pb.T / piece + 1) * pb.Hkv * pb.head_dim * pb.head_dim * sizeof(float);
+  // (work-items of a launch are counted in 32 bits)
+  if (piece > INT32_MAX / 2 || g->slots * pb.Hkv > (long long)UINT32_MAX / (2 * pb.head_dim) ||
+      (long long)pb.R * pb.Hkv > (long long)(UINT32_MAX / 256) / (pb.head_dim * pb.head_dim / 1024))
+    return UP_ERR_UNSUPPORTED;
+  return UP_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -131,7 +153,9 @@ int uniprefill_linear_attention_plan(const up_params* p, const int32_t* cu_seqle
   if (st != UP_OK) return st;
   if (workspace_bytes == nullptr) return UP_ERR_NULL;
   if ((st = check_cu(p, cu_seqlens_host)) != UP_OK) return st;
-  *workspace_bytes = 0;
+  LinearGeometry g;
+  if ((st = linear_geometry(pb, cu_seqlens_host, &g)) != UP_OK) return st;
+  *workspace_bytes = g.total;
   return UP_OK;
 }
 
@@ -146,10 +170,15 @@ int uniprefill_linear_attention(const up_params* p, const void* q, const void* k
   if (st != UP_OK) return st;
   if (!cu_seqlens_dev) return UP_ERR_NULL;
   if ((st = check_cu(p, cu_seqlens_host)) != UP_OK) return st;
-  (void)workspace; (void)workspace_bytes;
+  LinearGeometry g;
+  if ((st = linear_geometry(pb, cu_seqlens_host, &g)) != UP_OK) return st;
+  if (g.total > 0 && (workspace == nullptr || workspace_bytes < g.total)) return UP_ERR_WORKSPACE;
+  if (g.total > 0 && !aligned_to(workspace, 256)) return UP_ERR_ALIGN;
   if (pb.R == 0) return UP_OK;
   a.cu = cu_seqlens_dev;
-  return launch_linear_tokens(a, pb.qk_is_f32, pb.head_dim, (hipStream_t)stream) == hipSuccess ? UP_OK : UP_ERR_HIP;
+  a.piece = g.piece; a.slots = (int)g.slots;
+  if (g.total > 0) a.adds = (float*)workspace;
+  return launch_linear(a, pb.qk_is_f32, pb.head_dim, (hipStream_t)stream) == hipSuccess ? UP_OK : UP_ERR_HIP;
 }
 
 int uniprefill_linear_attention_step(const up_params* p, const void* q, const void* k, const void* v, int64_t v_row_stride,

@@ -86,6 +86,361 @@ __global__ __launch_bounds__(256) void k_linear_tokens(LinearArgs a) {
   }
 }
 
+// ---- chunks
+//
+// Chunks of 32 tokens: with i, j the tokens' places in the chunk and S the state before it,
+//     out_i = scale (lam^(i+1) q_i S + sum_{j<=i} lam^(i-j) <q_i, k_j> v_j),       S <- lam^m S + sum_j k_j^T (lam^(m-1-j) v_j)
+// (m tokens in the chunk).  A work-group walks over the chunks of one kv head, a wave holding 32 columns of the state in accumulators;
+// all the wave's products have its columns as lanes or rows, so that waves share tiles of q, k and v in LDS and nothing else:
+//     P^T = K Q^T,    O^T = S^T Q^T (scaled) + V^T P^T,    S += K^T V'
+// P^T and S leave the matrix cores in the layout that an operand of the next product has: the contraction takes keys (elements of a key)
+// in the order in which the lanes hold them.  K^T and V^T come out of row-major LDS through the transposing read.
+//
+// Products of bf16 are exact and summed in float.  What is scaled first is no bf16 any more: P and S enter the products for the outputs
+// in two parts of bf16 (16 bits), V' the one for the state in three (24 bits: what the state adds up over a long sequence stays float).
+//
+// Long sequences are cut into pieces of `piece` tokens: one launch leaves what every piece adds to the state, a second
+// adds these up in order, and the third walks over the pieces from the states that they begin with.
+constexpr int kLinearChunk = 32;
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ unsigned linear_pack(float a, float b) {
+  const f32x2 v = {a, b};
+  return __builtin_bit_cast(unsigned, __builtin_convertvector(v, bf16x2));
+}
+__device__ __forceinline__ float low_half(unsigned w) { return __builtin_bit_cast(float, w << 16); }
+__device__ __forceinline__ float high_half(unsigned w) { return __builtin_bit_cast(float, w & 0xFFFF0000u); }
+// eight floats in one part of bf16, and what is left of them
+__device__ __forceinline__ u32x4 linear_part(float* x) {
+  u32x4 w;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    w[i] = linear_pack(x[2 * i], x[2 * i + 1]);
+    x[2 * i] -= low_half(w[i]);
+    x[2 * i + 1] -= high_half(w[i]);
+  }
+  return w;
+}
+__device__ __forceinline__ f32x16 linear_mfma(const u32x4& a, const u32x4& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 linear_mfma(float a, float b, const f32x16& c) { return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0); }
+
+// Tiles in LDS: 32 rows of PPR pieces of 16 bytes, the pieces of a row permuted so that both 16 rows' same piece and 4 rows' neighbouring
+// pieces lie in different banks.
+template <int PPR>
+__device__ __forceinline__ int linear_swap(int row) { return PPR == 8 ? ((row & 2) << 1) | ((row >> 2) & 3) : ((row & 3) << 2) | ((row >> 2) & 3); }
+
+template <bool F32, int D>
+struct LinearTile {
+  static constexpr int WAVES = D / 32, THREADS = 64 * WAVES, SRCB = D * (F32 ? 4 : 2), PPR = SRCB / 16;
+  static constexpr int LOADS = kLinearChunk * PPR / THREADS;      // pieces per thread and tile
+  static constexpr int KT = D / 32;                               // tiles of 32 elements along a key
+};
+
+// place of a piece of the work: sequence r from its token t0 on, at most `piece` tokens
+struct LinearPiece {
+  int r, index, t0, tokens, length;      // t0: in the sequence; length: the sequence's
+};
+__device__ __forceinline__ bool linear_locate(const LinearArgs& a, int slot, LinearPiece& w) {
+  w.r = locate_slot(a.cu, a.R, a.piece, slot);
+  w.index = slot - slot_base(a.cu[w.r], w.r, a.piece);
+  w.length = a.cu[w.r + 1] - a.cu[w.r];
+  w.t0 = w.index * a.piece;
+  w.tokens = imin(a.piece, w.length - w.t0);
+  return w.tokens > 0 || w.index == 0;      // (a sequence without tokens hands its state on)
+}
+// what the piece adds (and later the state it begins with), in the workspace: sequences that are cut are longer than a piece, so they own
+// floor(2 cu / piece) .. and as many as they have pieces
+__device__ __forceinline__ float* linear_add(const LinearArgs& a, const LinearPiece& w, int D) {
+  return a.adds + (2ll * a.cu[w.r] / a.piece + w.index) * a.Hkv * D * D;
+}
+
+template <bool F32, int D, bool OUT>
+__global__ __launch_bounds__(64 * (D / 32), 2) void k_linear(LinearArgs a) {
+  typedef LinearTile<F32, D> T;
+  __shared__ __align__(16) u32x4 sk[kLinearChunk * T::PPR], sv[kLinearChunk * T::PPR], sq[OUT ? kLinearChunk * T::PPR : 1];
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int kvh = blockIdx.x % a.Hkv;
+  LinearPiece w;
+  if (!linear_locate(a, blockIdx.x / a.Hkv, w)) return;
+  const bool cut = w.length > a.piece;
+  const long long to = linear_slot(a.state_out, w.r, a.num_states);
+  if (!OUT && (!cut || (w.t0 + w.tokens == w.length && to < 0))) return;      // (nobody asks for what the last piece adds)
+  const long long first = (long long)a.cu[w.r] + w.t0;
+  const float ld = fminf(fmaxf(a.log_decay[kvh], -1e4f), 0.0f) * 1.44269504088896340736f;
+
+  // ---- the state: element e of S[kt] is row 32 kt + 8 (e / 4) + 4 half + e % 4, column 32 wave + l32
+  const long long state_at = (long long)kvh * D * D + 4 * half * D + 32 * wave + l32;
+  f32x16 S[T::KT];
+  const float* from = nullptr;
+  if (OUT && cut) from = linear_add(a, w, D);
+  if (OUT && !cut) {
+    const long long slot = linear_slot(a.state_in, w.r, a.num_states);
+    if (slot >= 0) from = a.states + slot * a.state_stride;
+  }
+#pragma unroll
+  for (int kt = 0; kt < T::KT; ++kt)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) S[kt][e] = from != nullptr ? from[state_at + (32 * kt + 8 * (e >> 2) + (e & 3)) * D] : 0.0f;
+
+  // ---- weights: of the logits (token l32 against token 8 (e / 4) + 4 half + e % 4), of the values, of the state
+  auto key_of = [&](int e) { return 8 * (e >> 2) + 4 * half + (e & 3); };
+  float wp[OUT ? 16 : 1], wv[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    if (OUT) wp[e] = key_of(e) <= l32 ? __builtin_amdgcn_exp2f(ld * (float)(l32 - key_of(e))) : 0.0f;
+    wv[e] = __builtin_amdgcn_exp2f(ld * (float)(kLinearChunk - 1 - key_of(e)));
+  }
+  const float wo = __builtin_amdgcn_exp2f(ld * (float)(l32 + 1));
+  float hi, lo;
+  linear_decay(a.log_decay[kvh], kLinearChunk, hi, lo);
+
+  // ---- tiles: fetched into registers while the ones before them are worked on
+  u32x4 rk[T::LOADS], rv[T::LOADS], rq[OUT ? T::LOADS : 1];
+  auto fetch = [&](const char* base, long long stride, int c0, u32x4* reg) {
+#pragma unroll
+    for (int i = 0; i < T::LOADS; ++i) {
+      const int at = i * T::THREADS + tid, row = imin(c0 + at / T::PPR, w.tokens - 1);      // (rows past the end repeat the last one)
+      reg[i] = *(const u32x4*)(base + (first + row) * stride + (at % T::PPR) * 16);
+    }
+  };
+  auto put = [&](const u32x4* reg, u32x4* tile) {
+#pragma unroll
+    for (int i = 0; i < T::LOADS; ++i) {
+      const int at = i * T::THREADS + tid, row = at / T::PPR;
+      tile[row * T::PPR + ((at % T::PPR) ^ linear_swap<T::PPR>(row))] = reg[i];
+    }
+  };
+  const char* kbase = a.k + (long long)kvh * T::SRCB;
+  const char* vbase = a.v + (long long)kvh * T::SRCB;
+  const char* qbase = a.q + (long long)kvh * a.Gq * T::SRCB;
+  // Operands out of LDS.  row_part: eight elements 32 kt + 16 st + {4 half .. +3, 8 + 4 half .. +3} of row l32 (bf16); four elements
+  // 32 kt + 8 j + 4 half .. of it (float).  column_part: column 32 kt + l32 of the tile's rows 16 st + {4 half .. +3, 8 + 4 half .. +3}.
+  // The place of a piece is that of piece 0 with the piece's bits turned over: one address a lane and an exclusive or each.
+  unsigned row_at = l32 * T::SRCB + ((linear_swap<T::PPR>(l32) ^ (F32 ? half : 0)) * 16) + (F32 ? 0 : 8 * half);
+  const int trow = 4 * half + ((lane >> 2) & 3), tpiece = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+  unsigned col_at = F32 ? 4 * half * T::SRCB + (((l32 >> 2) ^ half) * 16) + (l32 & 3) * 4
+                        : trow * T::SRCB + ((tpiece ^ linear_swap<T::PPR>(trow)) * 16) + (lane & 1) * 8;
+  auto row_part = [&](const u32x4* tile, int piece) __attribute__((always_inline)) {
+    if (F32) return *(const u32x4*)((const char*)tile + (row_at ^ (piece * 16)));
+    const u32x2 x = *(const u32x2*)((const char*)tile + (row_at ^ (piece * 16))), y = *(const u32x2*)((const char*)tile + (row_at ^ ((piece + 1) * 16)));
+    return u32x4{x.x, x.y, y.x, y.y};
+  };
+  auto column_part = [&](const u32x4* tile, int kt, int st) __attribute__((always_inline)) {
+    typedef __attribute__((address_space(3))) s16x4* lds4;
+    auto at = [&](unsigned flip, int row) { return (lds4)(__attribute__((address_space(3))) char*)((const char*)tile + (col_at ^ (kt * 64) ^ flip) + row * T::SRCB); };
+    const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(0, 16 * st)));
+    const u32x2 y = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(32, 16 * st + 8)));      // (8 rows on, a swap's bit 1 is the other)
+    return u32x4{x.x, x.y, y.x, y.y};
+  };
+  auto column_float = [&](const u32x4* tile, int kt, int e) __attribute__((always_inline)) {      // column 32 kt + l32 of row key_of(e)
+    const int swap = ((e & 3) << 2) | ((2 * (e >> 2)) & 3);
+    return *(const float*)((const char*)tile + (col_at ^ (kt * 128) ^ (swap * 16)) + (8 * (e >> 2) + (e & 3)) * T::SRCB);
+  };
+
+  if (w.tokens > 0) {
+    fetch(kbase, a.k_stride_b, 0, rk);
+    fetch(vbase, a.v_stride_b, 0, rv);
+    if (OUT) fetch(qbase, a.q_stride_b, 0, rq);
+    put(rk, sk);
+    put(rv, sv);
+    if (OUT) put(rq, sq);
+    __syncthreads();
+  }
+  for (int c0 = 0; c0 < w.tokens; c0 += kLinearChunk) {
+    const int m = imin(kLinearChunk, w.tokens - c0);
+    const bool last_chunk = c0 + kLinearChunk >= w.tokens;
+    if (m < kLinearChunk) {      // the last chunk is short: other weights
+#pragma unroll
+      for (int e = 0; e < 16; ++e) wv[e] = key_of(e) < m ? __builtin_amdgcn_exp2f(ld * (float)(m - 1 - key_of(e))) : 0.0f;
+      linear_decay(a.log_decay[kvh], m, hi, lo);
+    }
+    for (int g = 0; g < (OUT ? a.Gq : 1); ++g) {
+      const bool last_head = !OUT || g == a.Gq - 1;
+      if (last_head && !last_chunk) {
+        fetch(kbase, a.k_stride_b, c0 + kLinearChunk, rk);
+        fetch(vbase, a.v_stride_b, c0 + kLinearChunk, rv);
+        if (OUT) fetch(qbase, a.q_stride_b, c0 + kLinearChunk, rq);
+      }
+      if (OUT && !last_head) fetch(qbase + (g + 1) * T::SRCB, a.q_stride_b, c0, rq);
+      // (made anew in every round: kept over the loops, addresses and the state's parts would push accumulators into scratch)
+      asm volatile("" : "+v"(row_at), "+v"(col_at));
+#pragma unroll
+      for (int kt = 0; kt < T::KT; ++kt) asm volatile("" : "+v"(S[kt]));
+      if constexpr (OUT) {
+        f32x16 P, O;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) P[e] = O[e] = 0.0f;
+#pragma unroll
+        for (int kt = 0; kt < T::KT; ++kt) {
+          if constexpr (F32) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const u32x4 q4 = row_part(sq, 8 * kt + 2 * j), k4 = row_part(sk, 8 * kt + 2 * j);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float qf = __builtin_bit_cast(float, (unsigned)q4[i]), kf = __builtin_bit_cast(float, (unsigned)k4[i]);
+                P = linear_mfma(kf, qf, P);
+                O = linear_mfma(S[kt][4 * j + i], qf, O);
+              }
+            }
+          } else {
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+              const u32x4 q8 = row_part(sq, 4 * kt + 2 * st), k8 = row_part(sk, 4 * kt + 2 * st);
+              P = linear_mfma(k8, q8, P);
+              float x[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) x[i] = S[kt][8 * st + i];
+              const u32x4 s1 = linear_part(x), s2 = linear_part(x);
+              O = linear_mfma(s1, q8, O);
+              O = linear_mfma(s2, q8, O);
+            }
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          P[e] *= wp[e];
+          O[e] *= wo;
+        }
+        if constexpr (F32) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) O = linear_mfma(column_float(sv, wave, e), P[e], O);
+        } else {
+#pragma unroll
+          for (int st = 0; st < 2; ++st) {
+            const u32x4 v8 = column_part(sv, wave, st);
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = P[8 * st + i];
+            const u32x4 p1 = linear_part(x), p2 = linear_part(x);
+            O = linear_mfma(v8, p1, O);
+            O = linear_mfma(v8, p2, O);
+          }
+        }
+        if (l32 < m) {      // element e of O: token l32, column 32 wave + 8 (e / 4) + 4 half + e % 4
+          char* dst = a.out + (first + c0 + l32) * a.out_stride_b + (long long)(kvh * a.Gq + g) * T::SRCB;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int col = 32 * wave + 8 * j + 4 * half;
+            const float x0 = O[4 * j] * a.scale, x1 = O[4 * j + 1] * a.scale, x2 = O[4 * j + 2] * a.scale, x3 = O[4 * j + 3] * a.scale;
+            if (F32) *(f32x4*)(dst + col * 4) = f32x4{x0, x1, x2, x3};
+            else *(u32x2*)(dst + col * 2) = u32x2{linear_pack(x0, x1), linear_pack(x2, x3)};
+          }
+        }
+      }
+      if (last_head) {      // the state goes past the chunk
+#pragma unroll
+        for (int kt = 0; kt < T::KT; ++kt)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) S[kt][e] = fmaf(S[kt][e], hi, S[kt][e] * lo);
+        if constexpr (F32) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float x = column_float(sv, wave, e) * wv[e];
+#pragma unroll
+            for (int kt = 0; kt < T::KT; ++kt) S[kt] = linear_mfma(column_float(sk, kt, e), x, S[kt]);
+          }
+        } else {
+#pragma unroll
+          for (int st = 0; st < 2; ++st) {
+            const u32x4 v8 = column_part(sv, wave, st);
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              x[2 * i] = low_half(v8[i]) * wv[8 * st + 2 * i];
+              x[2 * i + 1] = high_half(v8[i]) * wv[8 * st + 2 * i + 1];
+            }
+            const u32x4 v1 = linear_part(x), v2 = linear_part(x), v3 = linear_part(x);
+#pragma unroll
+            for (int kt = 0; kt < T::KT; ++kt) {
+              const u32x4 k8 = column_part(sk, kt, st);
+              S[kt] = linear_mfma(k8, v1, S[kt]);
+              S[kt] = linear_mfma(k8, v2, S[kt]);
+              S[kt] = linear_mfma(k8, v3, S[kt]);
+            }
+          }
+        }
+      }
+      __syncthreads();
+      if (last_head && !last_chunk) {
+        put(rk, sk);
+        put(rv, sv);
+      }
+      if (OUT && !(last_head && last_chunk)) put(rq, sq);
+      __syncthreads();
+    }
+  }
+  float* dst = !OUT ? linear_add(a, w, D) : !cut && to >= 0 ? a.states + to * a.state_stride : nullptr;
+  if (dst != nullptr) {
+#pragma unroll
+    for (int kt = 0; kt < T::KT; ++kt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) dst[state_at + (32 * kt + 8 * (e >> 2) + (e & 3)) * D] = S[kt][e];
+  }
+}
+
+// The states that the pieces of cut sequences begin with, from what every piece adds, in order; and the state afterwards.
+template <int D>
+__global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
+  constexpr int PARTS = D * D / 1024;
+  const int part = blockIdx.x % PARTS, kvh = (blockIdx.x / PARTS) % a.Hkv;
+  LinearPiece w;
+  w.r = blockIdx.x / (PARTS * a.Hkv);
+  w.length = a.cu[w.r + 1] - a.cu[w.r];
+  w.index = 0;
+  if (w.length <= a.piece) return;
+  const long long at = (long long)kvh * D * D + part * 1024 + threadIdx.x * 4, step = (long long)a.Hkv * D * D;
+  const long long from = linear_slot(a.state_in, w.r, a.num_states), to = linear_slot(a.state_out, w.r, a.num_states);
+  f32x4 S = {0, 0, 0, 0};
+  if (from >= 0) S = *(const f32x4*)(a.states + from * a.state_stride + at);
+  float* add = linear_add(a, w, D) + at;
+  float hi, lo;
+  linear_decay(a.log_decay[kvh], a.piece, hi, lo);
+  int left = w.length;
+  for (; left > a.piece; left -= a.piece, add += step) {
+    const f32x4 x = *(const f32x4*)add;
+    *(f32x4*)add = S;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) S[e] = fmaf(S[e], hi, fmaf(S[e], lo, x[e]));
+  }
+  if (to >= 0) {
+    const f32x4 x = *(const f32x4*)add;
+    float h, l;
+    linear_decay(a.log_decay[kvh], left, h, l);
+    f32x4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = fmaf(S[e], h, fmaf(S[e], l, x[e]));
+    *(f32x4*)(a.states + to * a.state_stride + at) = y;
+  }
+  *(f32x4*)add = S;
+}
+
+template <bool F32, int D>
+static hipError_t launch_linear_form(const LinearArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)a.slots * a.Hkv), block(64 * (D / 32));
+  if (a.adds != nullptr) {
+    hipLaunchKernelGGL((k_linear<F32, D, false>), grid, block, 0, s, a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((k_linear_join<D>), dim3((unsigned)a.R * a.Hkv * (D * D / 1024)), dim3(256), 0, s, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL((k_linear<F32, D, true>), grid, block, 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_linear(const LinearArgs& a, bool f32, int D, hipStream_t s) {
+  if (f32) return D == 64 ? launch_linear_form<true, 64>(a, s) : launch_linear_form<true, 128>(a, s);
+  return D == 64 ? launch_linear_form<false, 64>(a, s) : D == 128 ? launch_linear_form<false, 128>(a, s) : launch_linear_form<false, 256>(a, s);
+}
+
 template <bool F32, int D>
 static hipError_t launch_linear_tokens_form(const LinearArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((k_linear_tokens<F32, D>), dim3((unsigned)a.R * a.Hkv * (D / 32)), dim3(256), 0, s, a);
