@@ -348,13 +348,22 @@ __global__ __launch_bounds__(64 * WAVES, (AttnTile<F32, D, WAVES>::DENSE)) void 
     }
     // element e of s[sub]: key k0 + 32*sub + 8*(e/4) + 4*half + e%4, row l32
     if (decltype(mask_tag)::value) {
+      const int ago = pos - k0 - 4 * half;      // how far the row is past the lane's first key
+      if (!WINDOW || k0 < a.n_sink) {
 #pragma unroll
-      for (int sub = 0; sub < T::SUB; ++sub)
+        for (int sub = 0; sub < T::SUB; ++sub)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int key = k0 + sub * 32 + 8 * (e >> 2) + 4 * half + (e & 3);
-          if (key > pos || (WINDOW && key <= pos - a.window && key >= a.n_sink)) s[sub][e] = -INFINITY;
-        }
+          for (int e = 0; e < 16; ++e) {
+            const int at = sub * 32 + 8 * (e >> 2) + (e & 3);
+            if (WINDOW ? ago < at || (ago - at >= a.window && k0 + 4 * half + at >= a.n_sink) : k0 + at + 4 * half > pos) s[sub][e] = -INFINITY;
+          }
+      } else if (k0 + T::KT - 1 > wave_first || k0 <= wave_last - a.window) {      // (one comparison for both ends of a window, in unsigned numbers)
+#pragma unroll
+        for (int sub = 0; sub < T::SUB; ++sub)
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if ((unsigned)(ago - (sub * 32 + 8 * (e >> 2) + (e & 3))) >= (unsigned)a.window) s[sub][e] = -INFINITY;
+      }
     }
     float mx = s[0][0];
 #pragma unroll
@@ -466,35 +475,49 @@ __global__ __launch_bounds__(64 * WAVES, (AttnTile<F32, D, WAVES>::DENSE)) void 
       if (key <= wave_last && k0 + u * T::KT < k_end) tile(std::true_type{}, key, sk + u * NEXT, sv + u * NEXT);
     }
   };
-  stage_any(key_at(k_begin), sk0, sv0);
-  staged();
-  int k0 = k_begin;
   if constexpr (WINDOW) {
-    // Stages that every row sees whole lie in the middle of the band, or among the sinks.
-    auto whole = [&](int place) {
-      const int key = key_at(place);
-      return place + T::KS <= k_end && key + T::KS - 1 <= pos0 && (key > last_pos - a.window || key + T::KS <= a.n_sink);
+    // Stages that every row sees whole lie among the sinks ([s0, s1)) and in the middle of the band ([s2, s3)); the sums do not ask for
+    // an order, so these come first, as q = 0 .. n_whole - 1, and the stages that need the masks after them.  (In one loop that chose
+    // between the two ways to stage, and between masks and none, the registers of the 256-wide kernel spilled 800 times, 2297 us for a
+    // prompt of 32768 with a window of 4096 against 1965; and where the branches of a stage ended in the same loads, the compiler had
+    // one of them load from an address that it had not set.)
+    const int first = k_begin / T::KS, last = (k_end + T::KS - 1) / T::KS;
+    auto within = [&](int place) { return imax(first, imin(last, place / T::KS)); };
+    const int band_whole = band.sinks + imax(0, last_pos - a.window + 1 - band.low + T::KS - 1);      // (rounded up: places from here on are in every window)
+    const int s1 = within(imin(a.n_sink, pos0 + 1)), s2 = imax(s1, within(band_whole));
+    const int s3 = imax(s2, within(imin(k_end, band.sinks + pos0 + 1 - band.low)));
+    const int n_sinks = s1 - first, n_whole = n_sinks + s3 - s2;
+    auto place_of = [&](int q) {
+      const int i = q - n_whole, s = q < n_sinks ? first + q : q < n_whole ? s2 + q - n_sinks : i < s2 - s1 ? s1 + i : s3 + i - (s2 - s1);
+      return s * T::KS;
     };
-    auto stage = [&](int place, u32x4* sk, u32x4* sv) __attribute__((always_inline)) {
-      if (place >= k_end) return;
-      const int key = key_at(place);
-      if (in_runs && key + T::KS <= Lk && (key >= band_first || key + T::KS <= a.n_sink)) stage_run(key, sk, sv);
-      else stage_any(key, sk, sv);
-    };
-    auto tiles = [&](int place, const u32x4* sk, const u32x4* sv) __attribute__((always_inline)) {
-      if (whole(place)) whole_tiles(key_at(place), sk, sv);
-      else last_tiles(place, sk, sv);
-    };
-    for (; k0 < k_end; k0 += 2 * T::KS) {
-      stage(k0 + T::KS, sk1, sv1);
-      tiles(k0, sk0, sv0);
+    const int n = last - first;
+    stage_any(key_at(place_of(0)), sk0, sv0);
+    staged();
+    int q = 0;
+    if (in_runs) {
+      for (; q + 2 < n_whole; q += 2) {
+        stage_run(key_at(place_of(q + 1)), sk1, sv1);
+        whole_tiles(key_at(place_of(q)), sk0, sv0);
+        staged();
+        stage_run(key_at(place_of(q + 2)), sk0, sv0);
+        whole_tiles(key_at(place_of(q + 1)), sk1, sv1);
+        staged();
+      }
+    }
+    for (; q < n; q += 2) {
+      if (q + 1 < n) stage_any(key_at(place_of(q + 1)), sk1, sv1);
+      last_tiles(place_of(q), sk0, sv0);
       staged();
-      if (k0 + T::KS >= k_end) break;
-      stage(k0 + 2 * T::KS, sk0, sv0);
-      tiles(k0 + T::KS, sk1, sv1);
+      if (q + 1 >= n) break;
+      if (q + 2 < n) stage_any(key_at(place_of(q + 2)), sk0, sv0);
+      last_tiles(place_of(q + 1), sk1, sv1);
       staged();
     }
   } else {
+  stage_any(k_begin, sk0, sv0);
+  staged();
+  int k0 = k_begin;
   const int whole = in_runs ? imin(imin(k_end, pos0 + 1), Lk - T::KS) - T::KS : k_begin - 1;
   for (; k0 + T::KS <= whole; k0 += 2 * T::KS) {
     stage_run(k0 + T::KS, sk1, sv1);
