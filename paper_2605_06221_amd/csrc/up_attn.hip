@@ -357,7 +357,7 @@ __global__ __launch_bounds__(64 * WAVES, (AttnTile<F32, D, WAVES>::DENSE)) void 
             const int at = sub * 32 + 8 * (e >> 2) + (e & 3);
             if (WINDOW ? ago < at || (ago - at >= a.window && k0 + 4 * half + at >= a.n_sink) : k0 + at + 4 * half > pos) s[sub][e] = -INFINITY;
           }
-      } else if (k0 + T::KT - 1 > wave_first || k0 <= wave_last - a.window) {      // (one comparison for both ends of a window, in unsigned numbers)
+      } else {      // (one comparison for both ends of a window, in unsigned numbers)
 #pragma unroll
         for (int sub = 0; sub < T::SUB; ++sub)
 #pragma unroll
