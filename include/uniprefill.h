@@ -682,8 +682,9 @@ int uniprefill_attention_window_step(const up_params* p, const void* q, const vo
  *   out          as for uniprefill_attention; overlaps none of q, k, v
  *   workspace    from uniprefill_linear_attention_plan with the same lengths
  *                (256-byte aligned; 0 bytes, and NULL, where no sequence is cut)
- * Refusals as for uniprefill_attention; more than (2^32 - 1) / 256 work-groups of 32
- * state columns: UP_ERR_UNSUPPORTED. */
+ * Refusals as for uniprefill_attention; rows (of q and out too) more than 2^27 bytes apart, and
+ * more than (2^32 - 1) / 256 work-groups (num_seqs * num_kv_heads * (head_dim / 32)^2 of them at most):
+ * UP_ERR_UNSUPPORTED. */
 int uniprefill_linear_attention_plan(const up_params* p, const int32_t* cu_seqlens_host, size_t* workspace_bytes);
 int uniprefill_linear_attention(const up_params* p, const void* q, const void* k, const void* v, int64_t v_row_stride,
                                 const int32_t* cu_seqlens_dev, const int32_t* cu_seqlens_host, const float* log_decay,

@@ -30,6 +30,10 @@ int linear_args(const up_params* p, const void* q, const void* k, const void* v,
   if ((st = check_row_stride(v_row_stride, pb->Hkv, pb->head_dim, e)) != UP_OK) return st;
   if ((st = check_row_stride(out_row_stride, pb->Hq, pb->head_dim, e)) != UP_OK) return st;
   if (any_state && num_states > 0 && state_stride > kMostStride / num_states) return UP_ERR_UNSUPPORTED;
+  // (offsets of a chunk's rows stay within 32 bits)
+  if (pb->q_stride * e > kMaxRowStride || pb->k_stride * e > kMaxRowStride || v_row_stride * e > kMaxRowStride ||
+      out_row_stride * e > kMaxRowStride)
+    return UP_ERR_UNSUPPORTED;
   if (any_state && num_states > 0 && state_stride % 4 != 0) return UP_ERR_ALIGN;
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(states)) return UP_ERR_ALIGN;
   if (!aligned_to(log_decay, 4) || !aligned_to(state_in, 4) || !aligned_to(state_out, 4)) return UP_ERR_ALIGN;

@@ -10,11 +10,12 @@ __device__ __forceinline__ float linear_load(const char* p, int i, bool f32) {
   return f32 ? ((const float*)p)[i] : __builtin_bit_cast(float, (unsigned)((const unsigned short*)p)[i] << 16);
 }
 
-// exp(log_decay * n) as the sum of two floats: a state is scaled once per step, and the error of one float would add up over the steps
-__device__ __forceinline__ void linear_decay(float log_decay, int n, float& hi, float& lo) {
+// exp(log_decay * n) as a float and what it lacks, relative to it: a state is scaled once per step, and the error of one float would add
+// up over the steps
+__device__ __forceinline__ void linear_decay(float log_decay, int n, float& one, float& lacks) {
   const double x = exp((double)fminf(fmaxf(log_decay, -1e4f), 0.0f) * (double)n);
-  hi = (float)x;
-  lo = (float)(x - (double)hi);
+  one = (float)x;
+  lacks = one > 1e-30f ? (float)((x - (double)one) / (double)one) : 0.0f;
 }
 
 __device__ __forceinline__ long long linear_slot(const int32_t* of, int r, long long num) {
@@ -38,8 +39,9 @@ __global__ __launch_bounds__(256) void k_linear_tokens(LinearArgs a) {
     S[i] = f32x4{0, 0, 0, 0};
     if (from >= 0) S[i] = *(const f32x4*)(a.states + from * a.state_stride + ((long long)kvh * D + row0 + i) * D + col);
   }
-  float hi, lo;
-  linear_decay(a.log_decay[kvh], 1, hi, lo);
+  float one, lacks;
+  linear_decay(a.log_decay[kvh], 1, one, lacks);
+  const float hi = one, lo = one * lacks;
   int turn = 0;
   for (int t = c0; t < c0 + N; ++t) {
     const char* k = a.k + (long long)t * a.k_stride_b + (long long)kvh * D * E;
@@ -114,16 +116,20 @@ __device__ __forceinline__ unsigned linear_pack(float a, float b) {
 }
 __device__ __forceinline__ float low_half(unsigned w) { return __builtin_bit_cast(float, w << 16); }
 __device__ __forceinline__ float high_half(unsigned w) { return __builtin_bit_cast(float, w & 0xFFFF0000u); }
-// eight floats in one part of bf16, and what is left of them
+// Eight floats in one part of bf16, and what is left of them (exact).
 __device__ __forceinline__ u32x4 linear_part(float* x) {
   u32x4 w;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    w[i] = linear_pack(x[2 * i], x[2 * i + 1]);
-    x[2 * i] -= low_half(w[i]);
-    x[2 * i + 1] -= high_half(w[i]);
+    const unsigned part = linear_pack(x[2 * i], x[2 * i + 1]);
+    x[2 * i] -= low_half(part);
+    x[2 * i + 1] -= high_half(part);
+    w[i] = part;
   }
   return w;
+}
+__device__ __forceinline__ u32x4 linear_last_part(const float* x) {
+  return u32x4{linear_pack(x[0], x[1]), linear_pack(x[2], x[3]), linear_pack(x[4], x[5]), linear_pack(x[6], x[7])};
 }
 __device__ __forceinline__ f32x16 linear_mfma(const u32x4& a, const u32x4& b, const f32x16& c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -163,7 +169,8 @@ __device__ __forceinline__ float* linear_add(const LinearArgs& a, const LinearPi
 template <bool F32, int D, bool OUT>
 __global__ __launch_bounds__(64 * (D / 32), 2) void k_linear(LinearArgs a) {
   typedef LinearTile<F32, D> T;
-  __shared__ __align__(16) u32x4 sk[kLinearChunk * T::PPR], sv[kLinearChunk * T::PPR], sq[OUT ? kLinearChunk * T::PPR : 1];
+  constexpr int TILE = kLinearChunk * T::PPR;
+  __shared__ __align__(16) u32x4 tiles[2][(OUT ? 3 : 2) * TILE];      // keys and values (one of two by the chunk), queries (by the step)
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kvh = blockIdx.x % a.Hkv;
@@ -185,9 +192,15 @@ __global__ __launch_bounds__(64 * (D / 32), 2) void k_linear(LinearArgs a) {
     if (slot >= 0) from = a.states + slot * a.state_stride;
   }
 #pragma unroll
-  for (int kt = 0; kt < T::KT; ++kt)
+  for (int kt = 0; kt < T::KT; ++kt) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) S[kt][e] = from != nullptr ? from[state_at + (32 * kt + 8 * (e >> 2) + (e & 3)) * D] : 0.0f;
+    for (int e = 0; e < 16; ++e) S[kt][e] = 0.0f;
+    if (from != nullptr) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) S[kt][e] = from[state_at + (32 * kt + 8 * (e >> 2) + (e & 3)) * D];
+    }
+    __builtin_amdgcn_sched_barrier(0);      // (a tile's addresses at a time)
+  }
 
   // ---- weights: of the logits (token l32 against token 8 (e / 4) + 4 half + e % 4), of the values, of the state
   auto key_of = [&](int e) { return 8 * (e >> 2) + 4 * half + (e & 3); };
@@ -198,17 +211,27 @@ __global__ __launch_bounds__(64 * (D / 32), 2) void k_linear(LinearArgs a) {
     wv[e] = __builtin_amdgcn_exp2f(ld * (float)(kLinearChunk - 1 - key_of(e)));
   }
   const float wo = __builtin_amdgcn_exp2f(ld * (float)(l32 + 1));
-  float hi, lo;
-  linear_decay(a.log_decay[kvh], kLinearChunk, hi, lo);
+  // A chunk's decay; what the float lacks is made good every eighth chunk.
+  float decay, rest;
+  linear_decay(a.log_decay[kvh], kLinearChunk, decay, rest);
+  int owed = 0;
 
   // ---- tiles: fetched into registers while the ones before them are worked on
   u32x4 rk[T::LOADS], rv[T::LOADS], rq[OUT ? T::LOADS : 1];
-  auto fetch = [&](const char* base, long long stride, int c0, u32x4* reg) {
+  unsigned koff[T::LOADS], voff[T::LOADS], qoff[OUT ? T::LOADS : 1];
+  auto aim = [&](int rows) {      // rows past the end repeat the last one
 #pragma unroll
     for (int i = 0; i < T::LOADS; ++i) {
-      const int at = i * T::THREADS + tid, row = imin(c0 + at / T::PPR, w.tokens - 1);      // (rows past the end repeat the last one)
-      reg[i] = *(const u32x4*)(base + (first + row) * stride + (at % T::PPR) * 16);
+      const int at = i * T::THREADS + tid, row = imin(at / T::PPR, rows - 1);
+      koff[i] = (unsigned)row * (unsigned)a.k_stride_b + (at % T::PPR) * 16;
+      voff[i] = (unsigned)row * (unsigned)a.v_stride_b + (at % T::PPR) * 16;
+      if (OUT) qoff[i] = (unsigned)row * (unsigned)a.q_stride_b + (at % T::PPR) * 16;
     }
+  };
+  auto fetch = [&](const char* base, long long stride, int c0, const unsigned* off, u32x4* reg) __attribute__((always_inline)) {
+    const char* from_row = base + (first + c0) * stride;
+#pragma unroll
+    for (int i = 0; i < T::LOADS; ++i) reg[i] = *(const u32x4*)(from_row + off[i]);
   };
   auto put = [&](const u32x4* reg, u32x4* tile) {
 #pragma unroll
@@ -244,39 +267,78 @@ __global__ __launch_bounds__(64 * (D / 32), 2) void k_linear(LinearArgs a) {
     return *(const float*)((const char*)tile + (col_at ^ (kt * 128) ^ (swap * 16)) + (8 * (e >> 2) + (e & 3)) * T::SRCB);
   };
 
+  // S += K^T V'.  (Two parts would do in pieces whose state only makes outputs, but two paths cost a second state in registers.)
+  auto advance = [&](const u32x4* sk, const u32x4* sv) __attribute__((always_inline)) {
+            if constexpr (F32) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const float x = column_float(sv, wave, e) * wv[e];
+#pragma unroll
+                for (int kt = 0; kt < T::KT; ++kt) S[kt] = linear_mfma(column_float(sk, kt, e), x, S[kt]);
+              }
+            } else {
+#pragma unroll
+              for (int st = 0; st < 2; ++st) {
+                const u32x4 v8 = column_part(sv, wave, st);
+                float x[8];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  x[2 * i] = low_half(v8[i]) * wv[8 * st + 2 * i];
+                  x[2 * i + 1] = high_half(v8[i]) * wv[8 * st + 2 * i + 1];
+                }
+                const u32x4 v1 = linear_part(x), v2 = linear_part(x), v3 = linear_last_part(x);
+                u32x4 kc = column_part(sk, 0, st);
+#pragma unroll
+                for (int kt = 0; kt < T::KT; ++kt) {
+                  u32x4 kn = kc;
+                  if (kt + 1 < T::KT) kn = column_part(sk, kt + 1, st);
+                  S[kt] = linear_mfma(kc, v1, S[kt]);
+                  S[kt] = linear_mfma(kc, v2, S[kt]);
+                  S[kt] = linear_mfma(kc, v3, S[kt]);
+                  kc = kn;
+                }
+                __builtin_amdgcn_sched_barrier(0);
+              }
+            }
+  };
+
   if (w.tokens > 0) {
-    fetch(kbase, a.k_stride_b, 0, rk);
-    fetch(vbase, a.v_stride_b, 0, rv);
-    if (OUT) fetch(qbase, a.q_stride_b, 0, rq);
-    put(rk, sk);
-    put(rv, sv);
-    if (OUT) put(rq, sq);
+    aim(imin(kLinearChunk, w.tokens));
+    fetch(kbase, a.k_stride_b, 0, koff, rk);
+    fetch(vbase, a.v_stride_b, 0, voff, rv);
+    if (OUT) fetch(qbase, a.q_stride_b, 0, qoff, rq);
+    put(rk, tiles[0]);
+    put(rv, tiles[0] + TILE);
+    if (OUT) put(rq, tiles[0] + 2 * TILE);
     __syncthreads();
   }
+  int turn = 0, qturn = 0;
   for (int c0 = 0; c0 < w.tokens; c0 += kLinearChunk) {
     const int m = imin(kLinearChunk, w.tokens - c0);
     const bool last_chunk = c0 + kLinearChunk >= w.tokens;
     if (m < kLinearChunk) {      // the last chunk is short: other weights
 #pragma unroll
       for (int e = 0; e < 16; ++e) wv[e] = key_of(e) < m ? __builtin_amdgcn_exp2f(ld * (float)(m - 1 - key_of(e))) : 0.0f;
-      linear_decay(a.log_decay[kvh], m, hi, lo);
     }
     for (int g = 0; g < (OUT ? a.Gq : 1); ++g) {
       const bool last_head = !OUT || g == a.Gq - 1;
       if (last_head && !last_chunk) {
-        fetch(kbase, a.k_stride_b, c0 + kLinearChunk, rk);
-        fetch(vbase, a.v_stride_b, c0 + kLinearChunk, rv);
-        if (OUT) fetch(qbase, a.q_stride_b, c0 + kLinearChunk, rq);
+        if (w.tokens - c0 < 2 * kLinearChunk) aim(w.tokens - c0 - kLinearChunk);
+        fetch(kbase, a.k_stride_b, c0 + kLinearChunk, koff, rk);
+        fetch(vbase, a.v_stride_b, c0 + kLinearChunk, voff, rv);
+        if (OUT) fetch(qbase, a.q_stride_b, c0 + kLinearChunk, qoff, rq);
       }
-      if (OUT && !last_head) fetch(qbase + (g + 1) * T::SRCB, a.q_stride_b, c0, rq);
+      if (OUT && !last_head) fetch(qbase + (g + 1) * T::SRCB, a.q_stride_b, c0, qoff, rq);
       // (made anew in every round: kept over the loops, addresses and the state's parts would push accumulators into scratch)
       asm volatile("" : "+v"(row_at), "+v"(col_at));
 #pragma unroll
       for (int kt = 0; kt < T::KT; ++kt) asm volatile("" : "+v"(S[kt]));
+      const u32x4 *sk = tiles[turn], *sv = sk + TILE, *sq = tiles[qturn] + (OUT ? 2 * TILE : 0);
       if constexpr (OUT) {
         f32x16 P, O;
 #pragma unroll
         for (int e = 0; e < 16; ++e) P[e] = O[e] = 0.0f;
+        u32x4 q8[2][2], k8[2][2];      // (operands of one step are read while the one before is worked on; the barriers keep it at that)
 #pragma unroll
         for (int kt = 0; kt < T::KT; ++kt) {
           if constexpr (F32) {
@@ -291,17 +353,28 @@ __global__ __launch_bounds__(64 * (D / 32), 2) void k_linear(LinearArgs a) {
               }
             }
           } else {
+            if (kt == 0) {
+#pragma unroll
+              for (int st = 0; st < 2; ++st) { q8[0][st] = row_part(sq, 2 * st); k8[0][st] = row_part(sk, 2 * st); }
+            }
+            if (kt + 1 < T::KT) {
+#pragma unroll
+              for (int st = 0; st < 2; ++st) {
+                q8[(kt + 1) & 1][st] = row_part(sq, 4 * (kt + 1) + 2 * st);
+                k8[(kt + 1) & 1][st] = row_part(sk, 4 * (kt + 1) + 2 * st);
+              }
+            }
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
-              const u32x4 q8 = row_part(sq, 4 * kt + 2 * st), k8 = row_part(sk, 4 * kt + 2 * st);
-              P = linear_mfma(k8, q8, P);
+              P = linear_mfma(k8[kt & 1][st], q8[kt & 1][st], P);
               float x[8];
 #pragma unroll
               for (int i = 0; i < 8; ++i) x[i] = S[kt][8 * st + i];
-              const u32x4 s1 = linear_part(x), s2 = linear_part(x);
-              O = linear_mfma(s1, q8, O);
-              O = linear_mfma(s2, q8, O);
+              const u32x4 s1 = linear_part(x), s2 = linear_last_part(x);
+              O = linear_mfma(s1, q8[kt & 1][st], O);
+              O = linear_mfma(s2, q8[kt & 1][st], O);
             }
+            __builtin_amdgcn_sched_barrier(0);
           }
         }
 #pragma unroll
@@ -319,13 +392,13 @@ __global__ __launch_bounds__(64 * (D / 32), 2) void k_linear(LinearArgs a) {
             float x[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = P[8 * st + i];
-            const u32x4 p1 = linear_part(x), p2 = linear_part(x);
+            const u32x4 p1 = linear_part(x), p2 = linear_last_part(x);
             O = linear_mfma(v8, p1, O);
             O = linear_mfma(v8, p2, O);
           }
         }
         if (l32 < m) {      // element e of O: token l32, column 32 wave + 8 (e / 4) + 4 half + e % 4
-          char* dst = a.out + (first + c0 + l32) * a.out_stride_b + (long long)(kvh * a.Gq + g) * T::SRCB;
+          char* dst = a.out + (first + c0) * a.out_stride_b + (long long)(kvh * a.Gq + g) * T::SRCB + (unsigned)l32 * (unsigned)a.out_stride_b;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const int col = 32 * wave + 8 * j + 4 * half;
@@ -336,53 +409,41 @@ __global__ __launch_bounds__(64 * (D / 32), 2) void k_linear(LinearArgs a) {
         }
       }
       if (last_head) {      // the state goes past the chunk
+        float one = decay, lacks = 0.0f;      // (in place, and what is made good apart: two paths that end in other registers each cost a second state)
+        if (m < kLinearChunk) linear_decay(a.log_decay[kvh], m, one, lacks);
+        else if (++owed == 8) { lacks = 8.0f * rest; owed = 0; }
 #pragma unroll
         for (int kt = 0; kt < T::KT; ++kt)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) S[kt][e] = fmaf(S[kt][e], hi, S[kt][e] * lo);
-        if constexpr (F32) {
+          for (int e = 0; e < 16; ++e) S[kt][e] *= one;
+        if (lacks != 0.0f) {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float x = column_float(sv, wave, e) * wv[e];
+          for (int kt = 0; kt < T::KT; ++kt)
 #pragma unroll
-            for (int kt = 0; kt < T::KT; ++kt) S[kt] = linear_mfma(column_float(sk, kt, e), x, S[kt]);
-          }
-        } else {
-#pragma unroll
-          for (int st = 0; st < 2; ++st) {
-            const u32x4 v8 = column_part(sv, wave, st);
-            float x[8];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              x[2 * i] = low_half(v8[i]) * wv[8 * st + 2 * i];
-              x[2 * i + 1] = high_half(v8[i]) * wv[8 * st + 2 * i + 1];
-            }
-            const u32x4 v1 = linear_part(x), v2 = linear_part(x), v3 = linear_part(x);
-#pragma unroll
-            for (int kt = 0; kt < T::KT; ++kt) {
-              const u32x4 k8 = column_part(sk, kt, st);
-              S[kt] = linear_mfma(k8, v1, S[kt]);
-              S[kt] = linear_mfma(k8, v2, S[kt]);
-              S[kt] = linear_mfma(k8, v3, S[kt]);
-            }
-          }
+            for (int e = 0; e < 16; ++e) S[kt][e] = fmaf(S[kt][e], lacks, S[kt][e]);
         }
+        advance(sk, sv);
       }
-      __syncthreads();
+      // (into the buffers that were read a step ago: everyone is past that step's barrier)
+      qturn ^= 1;
       if (last_head && !last_chunk) {
-        put(rk, sk);
-        put(rv, sv);
+        turn ^= 1;
+        put(rk, tiles[turn]);
+        put(rv, tiles[turn] + TILE);
       }
-      if (OUT && !(last_head && last_chunk)) put(rq, sq);
+      if (OUT && !(last_head && last_chunk)) put(rq, tiles[qturn] + 2 * TILE);
       __syncthreads();
     }
   }
   float* dst = !OUT ? linear_add(a, w, D) : !cut && to >= 0 ? a.states + to * a.state_stride : nullptr;
   if (dst != nullptr) {
+    const float owes = (float)owed * rest;
 #pragma unroll
-    for (int kt = 0; kt < T::KT; ++kt)
+    for (int kt = 0; kt < T::KT; ++kt) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) dst[state_at + (32 * kt + 8 * (e >> 2) + (e & 3)) * D] = S[kt][e];
+      for (int e = 0; e < 16; ++e) dst[state_at + (32 * kt + 8 * (e >> 2) + (e & 3)) * D] = fmaf(S[kt][e], owes, S[kt][e]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
 }
 
@@ -401,22 +462,21 @@ __global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
   f32x4 S = {0, 0, 0, 0};
   if (from >= 0) S = *(const f32x4*)(a.states + from * a.state_stride + at);
   float* add = linear_add(a, w, D) + at;
-  float hi, lo;
-  linear_decay(a.log_decay[kvh], a.piece, hi, lo);
+  float one, lacks;
+  linear_decay(a.log_decay[kvh], a.piece, one, lacks);
   int left = w.length;
   for (; left > a.piece; left -= a.piece, add += step) {
     const f32x4 x = *(const f32x4*)add;
     *(f32x4*)add = S;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) S[e] = fmaf(S[e], hi, fmaf(S[e], lo, x[e]));
+    for (int e = 0; e < 4; ++e) S[e] = fmaf(S[e], one, fmaf(S[e], one * lacks, x[e]));
   }
   if (to >= 0) {
     const f32x4 x = *(const f32x4*)add;
-    float h, l;
-    linear_decay(a.log_decay[kvh], left, h, l);
+    linear_decay(a.log_decay[kvh], left, one, lacks);
     f32x4 y;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = fmaf(S[e], h, fmaf(S[e], l, x[e]));
+    for (int e = 0; e < 4; ++e) y[e] = fmaf(S[e], one, fmaf(S[e], one * lacks, x[e]));
     *(f32x4*)(a.states + to * a.state_stride + at) = y;
   }
   *(f32x4*)add = S;
