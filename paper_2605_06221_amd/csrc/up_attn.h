@@ -121,6 +121,12 @@ hipError_t launch_q4_load(const Q4CopyArgs& a, bool f32, hipStream_t s);
 hipError_t launch_q4_attention(const Q4AttnArgs& a, hipStream_t s);
 hipError_t launch_evict(const EvictArgs& a, hipStream_t s);
 
+// 16 bytes per lane from memory into 64 consecutive places of LDS that start at dst (the same for the whole wave)
+__device__ __forceinline__ void load_to_lds(const char* src, u32x4* dst) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                   (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+}
+
 // An entry of a block table at an index that is the same for the whole wave.  No kernel writes a table, so it may come through the
 // scalar cache: its wait is then not one for the vector loads in flight.
 __device__ __forceinline__ int table_entry(const int32_t* table, unsigned i) {

@@ -73,12 +73,6 @@ __device__ __forceinline__ int k_place(int row, int piece) { return row * PPR + 
 template <int PPR, bool F32>
 __device__ __forceinline__ int v_place(int row, int piece) { return row * PPR + (piece ^ v_swap<PPR, F32>(row)); }
 
-// 16 bytes per lane from memory into 64 consecutive places of LDS that start at dst (the same for the whole wave)
-__device__ __forceinline__ void load_to_lds(const char* src, u32x4* dst) {
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                   (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
-}
-
 __device__ __forceinline__ float attn_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // (by value: a bit cast straight from an element of a vector takes the vector's first)

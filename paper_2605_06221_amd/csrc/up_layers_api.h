@@ -49,7 +49,7 @@ int linear_args(const up_params* p, const void* q, const void* k, const void* v,
   return UP_OK;
 }
 
-// Sequences are cut into pieces of so many tokens that the batch makes about two work-groups for every CU (as many as its registers
+// Sequences are cut into pieces of so many tokens that the batch makes about three work-groups for every CU (as many as its registers
 // hold), none shorter than 256.
 struct LinearGeometry {
   int piece;
@@ -57,7 +57,7 @@ struct LinearGeometry {
   size_t total;
 };
 int linear_geometry(const Problem& pb, const int32_t* cu, LinearGeometry* g) {
-  long long piece = ((long long)pb.T * pb.Hkv / (2 * kCUs) + 63) / 64 * 64;
+  long long piece = ((long long)pb.T * pb.Hkv / (3 * kCUs) + 63) / 64 * 64;
   if (piece < 256) piece = 256;
   g->piece = (int)piece;
   g->slots = pb.T / piece + pb.R;

@@ -2,6 +2,7 @@
 //     S_t = lam S_{t-1} + k_t^T v_t,        out_t = scale q_t S_t      (S: D x D, float, carried by the sequence)
 //
 // k_linear_tokens, token after token: a work-group holds 32 columns of a head's state in registers, eight lanes by 32 groups of rows.
+#include "up_attn.h"
 #include "up_layers.h"
 
 namespace up {
@@ -146,6 +147,7 @@ struct LinearTile {
   static constexpr int WAVES = D / 32, THREADS = 64 * WAVES, SRCB = D * (F32 ? 4 : 2), PPR = SRCB / 16;
   static constexpr int LOADS = kLinearChunk * PPR / THREADS;      // pieces per thread and tile
   static constexpr int KT = D / 32;                               // tiles of 32 elements along a key
+  static constexpr int DENSE = D == 256 || F32 ? 2 : 3;           // waves per SIMD that the registers are held to
 };
 
 // place of a piece of the work: sequence r from its token t0 on, at most `piece` tokens
@@ -166,11 +168,20 @@ __device__ __forceinline__ float* linear_add(const LinearArgs& a, const LinearPi
   return a.adds + (2ll * a.cu[w.r] / a.piece + w.index) * a.Hkv * D * D;
 }
 
+// exp2(x * n), -120 <= x * n <= 0, to a float's rounding: a float's product would leave |x n| 2^-24 of error
+__device__ __forceinline__ float linear_power(double x, int n) {
+  const double y = x * (double)n, whole = rint(y);
+  return ldexpf(__builtin_amdgcn_exp2f((float)(y - whole)), (int)whole);
+}
+
 template <bool F32, int D, bool OUT>
-__global__ __launch_bounds__(64 * (D / 32), 2) void k_linear(LinearArgs a) {
+__global__ __launch_bounds__(64 * (D / 32), (LinearTile<F32, D>::DENSE)) void k_linear(LinearArgs a) {
   typedef LinearTile<F32, D> T;
   constexpr int TILE = kLinearChunk * T::PPR;
-  __shared__ __align__(16) u32x4 tiles[2][(OUT ? 3 : 2) * TILE];      // keys and values (one of two by the chunk), queries (by the step)
+  // keys, values and queries of a step, and of the next one.  (Two variables, not one array: the compiler then knows that a load into one and
+  // reads of the other do not meet, and does not wait for the load before them.)
+  __shared__ __align__(16) u32x4 tiles0[(OUT ? 3 : 2) * TILE], tiles1[(OUT ? 3 : 2) * TILE];
+  __shared__ __align__(16) float value_weight[kLinearChunk];
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kvh = blockIdx.x % a.Hkv;
@@ -178,9 +189,11 @@ __global__ __launch_bounds__(64 * (D / 32), 2) void k_linear(LinearArgs a) {
   if (!linear_locate(a, blockIdx.x / a.Hkv, w)) return;
   const bool cut = w.length > a.piece;
   const long long to = linear_slot(a.state_out, w.r, a.num_states);
-  if (!OUT && (!cut || (w.t0 + w.tokens == w.length && to < 0))) return;      // (nobody asks for what the last piece adds)
+  if (!OUT && !cut) return;
+  if (!OUT && w.t0 + w.tokens == w.length && to < 0) return;      // (nobody asks for what the last piece adds)
   const long long first = (long long)a.cu[w.r] + w.t0;
-  const float ld = fminf(fmaxf(a.log_decay[kvh], -1e4f), 0.0f) * 1.44269504088896340736f;
+  const double ld = (double)fminf(fmaxf(a.log_decay[kvh], -1e4f), 0.0f) * 1.4426950408889634074;
+  const float ldf = (float)ld;
 
   // ---- the state: element e of S[kt] is row 32 kt + 8 (e / 4) + 4 half + e % 4, column 32 wave + l32
   const long long state_at = (long long)kvh * D * D + 4 * half * D + 32 * wave + l32;
@@ -202,47 +215,51 @@ __global__ __launch_bounds__(64 * (D / 32), 2) void k_linear(LinearArgs a) {
     __builtin_amdgcn_sched_barrier(0);      // (a tile's addresses at a time)
   }
 
-  // ---- weights: of the logits (token l32 against token 8 (e / 4) + 4 half + e % 4), of the values, of the state
+  // ---- weights: of the logits (token l32 against token 8 (e / 4) + 4 half + e % 4), of the state's product, of the values
   auto key_of = [&](int e) { return 8 * (e >> 2) + 4 * half + (e & 3); };
-  float wp[OUT ? 16 : 1], wv[16];
+  float wp[OUT ? 16 : 1];
+  if (OUT) {
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    if (OUT) wp[e] = key_of(e) <= l32 ? __builtin_amdgcn_exp2f(ld * (float)(l32 - key_of(e))) : 0.0f;
-    wv[e] = __builtin_amdgcn_exp2f(ld * (float)(kLinearChunk - 1 - key_of(e)));
+    for (int e = 0; e < 16; ++e) wp[e] = key_of(e) <= l32 ? a.scale * __builtin_amdgcn_exp2f(ldf * (float)(l32 - key_of(e))) : 0.0f;
   }
-  const float wo = __builtin_amdgcn_exp2f(ld * (float)(l32 + 1));
-  // A chunk's decay; what the float lacks is made good every eighth chunk.
-  float decay, rest;
-  linear_decay(a.log_decay[kvh], kLinearChunk, decay, rest);
-  int owed = 0;
+  const float wo = a.scale * __builtin_amdgcn_exp2f(ldf * (float)(l32 + 1));
+  auto weigh = [&](int m) {      // (tokens past the chunk's m weigh nothing)
+    if (tid < kLinearChunk) value_weight[tid] = tid < m ? __builtin_amdgcn_exp2f(ldf * (float)(m - 1 - tid)) : 0.0f;
+  };
+  // The state stands in registers as S / f, f = lam^(tokens since they were last scaled): it is scaled when f has passed 2^-24, not with
+  // every chunk.
+  int since = 0;
+  float f = 1.0f;
 
-  // ---- tiles: fetched into registers while the ones before them are worked on
-  u32x4 rk[T::LOADS], rv[T::LOADS], rq[OUT ? T::LOADS : 1];
+  // ---- staging, straight from memory into LDS: a wave's load writes 64 consecutive places, WROWS rows; the permutation of a row's
+  // pieces is in the address that the lane reads
+  constexpr int WROWS = 64 / T::PPR, ROWSTEP = T::THREADS / T::PPR;
   unsigned koff[T::LOADS], voff[T::LOADS], qoff[OUT ? T::LOADS : 1];
   auto aim = [&](int rows) {      // rows past the end repeat the last one
 #pragma unroll
     for (int i = 0; i < T::LOADS; ++i) {
-      const int at = i * T::THREADS + tid, row = imin(at / T::PPR, rows - 1);
-      koff[i] = (unsigned)row * (unsigned)a.k_stride_b + (at % T::PPR) * 16;
-      voff[i] = (unsigned)row * (unsigned)a.v_stride_b + (at % T::PPR) * 16;
-      if (OUT) qoff[i] = (unsigned)row * (unsigned)a.q_stride_b + (at % T::PPR) * 16;
-    }
-  };
-  auto fetch = [&](const char* base, long long stride, int c0, const unsigned* off, u32x4* reg) __attribute__((always_inline)) {
-    const char* from_row = base + (first + c0) * stride;
-#pragma unroll
-    for (int i = 0; i < T::LOADS; ++i) reg[i] = *(const u32x4*)(from_row + off[i]);
-  };
-  auto put = [&](const u32x4* reg, u32x4* tile) {
-#pragma unroll
-    for (int i = 0; i < T::LOADS; ++i) {
-      const int at = i * T::THREADS + tid, row = at / T::PPR;
-      tile[row * T::PPR + ((at % T::PPR) ^ linear_swap<T::PPR>(row))] = reg[i];
+      const int row = i * ROWSTEP + wave * WROWS + lane / T::PPR, piece = (lane % T::PPR) ^ linear_swap<T::PPR>(row), at = imin(row, rows - 1);
+      koff[i] = (unsigned)at * (unsigned)a.k_stride_b + piece * 16;
+      voff[i] = (unsigned)at * (unsigned)a.v_stride_b + piece * 16;
+      if (OUT) qoff[i] = (unsigned)at * (unsigned)a.q_stride_b + piece * 16;
     }
   };
   const char* kbase = a.k + (long long)kvh * T::SRCB;
   const char* vbase = a.v + (long long)kvh * T::SRCB;
   const char* qbase = a.q + (long long)kvh * a.Gq * T::SRCB;
+  auto stage = [&](int c0, int g, u32x4* tiles) __attribute__((always_inline)) {
+    if (w.tokens - c0 < kLinearChunk) aim(w.tokens - c0);
+    const char* k = kbase + (first + c0) * a.k_stride_b;
+    const char* v = vbase + (first + c0) * a.v_stride_b;
+    const char* q = qbase + (first + c0) * a.q_stride_b + g * T::SRCB;
+#pragma unroll
+    for (int i = 0; i < T::LOADS; ++i) {
+      u32x4* to_row = tiles + (i * ROWSTEP + wave * WROWS) * T::PPR;
+      load_to_lds(k + koff[i], to_row);
+      load_to_lds(v + voff[i], to_row + TILE);
+      if (OUT) load_to_lds(q + qoff[i], to_row + 2 * TILE);
+    }
+  };
   // Operands out of LDS.  row_part: eight elements 32 kt + 16 st + {4 half .. +3, 8 + 4 half .. +3} of row l32 (bf16); four elements
   // 32 kt + 8 j + 4 half .. of it (float).  column_part: column 32 kt + l32 of the tile's rows 16 st + {4 half .. +3, 8 + 4 half .. +3}.
   // The place of a piece is that of piece 0 with the piece's bits turned over: one address a lane and an exclusive or each.
@@ -267,181 +284,163 @@ __global__ __launch_bounds__(64 * (D / 32), 2) void k_linear(LinearArgs a) {
     return *(const float*)((const char*)tile + (col_at ^ (kt * 128) ^ (swap * 16)) + (8 * (e >> 2) + (e & 3)) * T::SRCB);
   };
 
-  // S += K^T V'.  (Two parts would do in pieces whose state only makes outputs, but two paths cost a second state in registers.)
-  auto advance = [&](const u32x4* sk, const u32x4* sv) __attribute__((always_inline)) {
-            if constexpr (F32) {
+  // one head's outputs for the chunk
+  auto outputs = [&](int c0, int g, int m, const u32x4* sk, const u32x4* sv, const u32x4* sq) __attribute__((always_inline)) {
+    f32x16 P, O;
 #pragma unroll
-              for (int e = 0; e < 16; ++e) {
-                const float x = column_float(sv, wave, e) * wv[e];
+    for (int e = 0; e < 16; ++e) P[e] = O[e] = 0.0f;
 #pragma unroll
-                for (int kt = 0; kt < T::KT; ++kt) S[kt] = linear_mfma(column_float(sk, kt, e), x, S[kt]);
-              }
-            } else {
+    for (int kt = 0; kt < T::KT; ++kt) {
+      if constexpr (F32) {
 #pragma unroll
-              for (int st = 0; st < 2; ++st) {
-                const u32x4 v8 = column_part(sv, wave, st);
-                float x[8];
+        for (int j = 0; j < 4; ++j) {
+          const u32x4 q4 = row_part(sq, 8 * kt + 2 * j), k4 = row_part(sk, 8 * kt + 2 * j);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  x[2 * i] = low_half(v8[i]) * wv[8 * st + 2 * i];
-                  x[2 * i + 1] = high_half(v8[i]) * wv[8 * st + 2 * i + 1];
-                }
-                const u32x4 v1 = linear_part(x), v2 = linear_part(x), v3 = linear_last_part(x);
-                u32x4 kc = column_part(sk, 0, st);
+          for (int i = 0; i < 4; ++i) {
+            const float qf = __builtin_bit_cast(float, (unsigned)q4[i]), kf = __builtin_bit_cast(float, (unsigned)k4[i]);
+            P = linear_mfma(kf, qf, P);
+            O = linear_mfma(S[kt][4 * j + i], qf, O);
+          }
+        }
+      } else {
 #pragma unroll
-                for (int kt = 0; kt < T::KT; ++kt) {
-                  u32x4 kn = kc;
-                  if (kt + 1 < T::KT) kn = column_part(sk, kt + 1, st);
-                  S[kt] = linear_mfma(kc, v1, S[kt]);
-                  S[kt] = linear_mfma(kc, v2, S[kt]);
-                  S[kt] = linear_mfma(kc, v3, S[kt]);
-                  kc = kn;
-                }
-                __builtin_amdgcn_sched_barrier(0);
-              }
-            }
+        for (int st = 0; st < 2; ++st) {
+          const u32x4 q8 = row_part(sq, 4 * kt + 2 * st), k8 = row_part(sk, 4 * kt + 2 * st);
+          P = linear_mfma(k8, q8, P);
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = S[kt][8 * st + i];
+          const u32x4 s1 = linear_part(x), s2 = linear_last_part(x);
+          O = linear_mfma(s1, q8, O);
+          O = linear_mfma(s2, q8, O);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);      // (the operands of one step at a time: all of them at once push accumulators into scratch)
+    }
+    const float wof = wo * f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      P[e] *= wp[e];
+      O[e] *= wof;
+    }
+    if constexpr (F32) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) O = linear_mfma(column_float(sv, wave, e), P[e], O);
+    } else {
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        const u32x4 v8 = column_part(sv, wave, st);
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = P[8 * st + i];
+        const u32x4 p1 = linear_part(x), p2 = linear_last_part(x);
+        O = linear_mfma(v8, p1, O);
+        O = linear_mfma(v8, p2, O);
+      }
+    }
+    if (l32 < m) {      // element e of O: token l32, column 32 wave + 8 (e / 4) + 4 half + e % 4
+      char* dst = a.out + (first + c0) * a.out_stride_b + (long long)(kvh * a.Gq + g) * T::SRCB + (unsigned)l32 * (unsigned)a.out_stride_b;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int col = 32 * wave + 8 * j + 4 * half;
+        if (F32) *(f32x4*)(dst + col * 4) = f32x4{O[4 * j], O[4 * j + 1], O[4 * j + 2], O[4 * j + 3]};
+        else *(u32x2*)(dst + col * 2) = u32x2{linear_pack(O[4 * j], O[4 * j + 1]), linear_pack(O[4 * j + 2], O[4 * j + 3])};
+      }
+    }
+  };
+  // the state goes past the chunk: S += K^T V'.  In three parts where it is stored, in two where it only makes outputs.
+  auto advance = [&](int m, const u32x4* sk, const u32x4* sv) __attribute__((always_inline)) {
+    since += m;
+    f = ldf * (float)since > -120.0f ? linear_power(ld, since) : 0.0f;      // (what stands in S is up to 2^24 times the state)
+    f = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, f)));      // (the same for the whole wave: a branch)
+    if (f < 0x1p-24f) {
+#pragma unroll
+      for (int kt = 0; kt < T::KT; ++kt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) S[kt][e] *= f;
+      since = 0;
+      f = 1.0f;
+    }
+    const float inv = 1.0f / f;
+    if constexpr (F32) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float x = column_float(sv, wave, e) * (value_weight[key_of(e)] * inv);
+#pragma unroll
+        for (int kt = 0; kt < T::KT; ++kt) S[kt] = linear_mfma(column_float(sk, kt, e), x, S[kt]);
+      }
+    } else {
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        const u32x4 v8 = column_part(sv, wave, st);
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const f32x4 wv = *(const f32x4*)&value_weight[16 * st + 8 * i + 4 * half];
+          x[4 * i] = low_half(v8[2 * i]) * (wv[0] * inv);
+          x[4 * i + 1] = high_half(v8[2 * i]) * (wv[1] * inv);
+          x[4 * i + 2] = low_half(v8[2 * i + 1]) * (wv[2] * inv);
+          x[4 * i + 3] = high_half(v8[2 * i + 1]) * (wv[3] * inv);
+        }
+        const u32x4 v1 = linear_part(x), v2 = linear_part(x);
+#pragma unroll
+        for (int kt = 0; kt < T::KT; ++kt) {
+          const u32x4 k8 = column_part(sk, kt, st);
+          S[kt] = linear_mfma(k8, v1, S[kt]);
+          S[kt] = linear_mfma(k8, v2, S[kt]);
+          if (!OUT) S[kt] = linear_mfma(k8, linear_last_part(x), S[kt]);
+        }
+        if (OUT && !cut) {      // (a pass of its own, in place)
+          const u32x4 v3 = linear_last_part(x);
+#pragma unroll
+          for (int kt = 0; kt < T::KT; ++kt) S[kt] = linear_mfma(column_part(sk, kt, st), v3, S[kt]);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
   };
 
+  // ---- steps: a chunk and a query head each; the next one's tiles are loaded while one is worked on
   if (w.tokens > 0) {
     aim(imin(kLinearChunk, w.tokens));
-    fetch(kbase, a.k_stride_b, 0, koff, rk);
-    fetch(vbase, a.v_stride_b, 0, voff, rv);
-    if (OUT) fetch(qbase, a.q_stride_b, 0, qoff, rq);
-    put(rk, tiles[0]);
-    put(rv, tiles[0] + TILE);
-    if (OUT) put(rq, tiles[0] + 2 * TILE);
-    __syncthreads();
-  }
-  int turn = 0, qturn = 0;
-  for (int c0 = 0; c0 < w.tokens; c0 += kLinearChunk) {
-    const int m = imin(kLinearChunk, w.tokens - c0);
-    const bool last_chunk = c0 + kLinearChunk >= w.tokens;
-    if (m < kLinearChunk) {      // the last chunk is short: other weights
-#pragma unroll
-      for (int e = 0; e < 16; ++e) wv[e] = key_of(e) < m ? __builtin_amdgcn_exp2f(ld * (float)(m - 1 - key_of(e))) : 0.0f;
-    }
-    for (int g = 0; g < (OUT ? a.Gq : 1); ++g) {
+    weigh(imin(kLinearChunk, w.tokens));
+    int c0 = 0, g = 0;
+    auto step = [&](u32x4* here, u32x4* next) __attribute__((always_inline)) {      // false: the last one
       const bool last_head = !OUT || g == a.Gq - 1;
-      if (last_head && !last_chunk) {
-        if (w.tokens - c0 < 2 * kLinearChunk) aim(w.tokens - c0 - kLinearChunk);
-        fetch(kbase, a.k_stride_b, c0 + kLinearChunk, koff, rk);
-        fetch(vbase, a.v_stride_b, c0 + kLinearChunk, voff, rv);
-        if (OUT) fetch(qbase, a.q_stride_b, c0 + kLinearChunk, qoff, rq);
-      }
-      if (OUT && !last_head) fetch(qbase + (g + 1) * T::SRCB, a.q_stride_b, c0, qoff, rq);
-      // (made anew in every round: kept over the loops, addresses and the state's parts would push accumulators into scratch)
+      const int m = imin(kLinearChunk, w.tokens - c0), c1 = last_head ? c0 + kLinearChunk : c0, g1 = last_head ? 0 : g + 1;
+      const bool more = c1 < w.tokens;
+      if (more) stage(c1, g1, next);
+      // (made anew in every round: kept over the loop, addresses and the state's parts would push accumulators into scratch)
       asm volatile("" : "+v"(row_at), "+v"(col_at));
 #pragma unroll
       for (int kt = 0; kt < T::KT; ++kt) asm volatile("" : "+v"(S[kt]));
-      const u32x4 *sk = tiles[turn], *sv = sk + TILE, *sq = tiles[qturn] + (OUT ? 2 * TILE : 0);
-      if constexpr (OUT) {
-        f32x16 P, O;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) P[e] = O[e] = 0.0f;
-        u32x4 q8[2][2], k8[2][2];      // (operands of one step are read while the one before is worked on; the barriers keep it at that)
-#pragma unroll
-        for (int kt = 0; kt < T::KT; ++kt) {
-          if constexpr (F32) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const u32x4 q4 = row_part(sq, 8 * kt + 2 * j), k4 = row_part(sk, 8 * kt + 2 * j);
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const float qf = __builtin_bit_cast(float, (unsigned)q4[i]), kf = __builtin_bit_cast(float, (unsigned)k4[i]);
-                P = linear_mfma(kf, qf, P);
-                O = linear_mfma(S[kt][4 * j + i], qf, O);
-              }
-            }
-          } else {
-            if (kt == 0) {
-#pragma unroll
-              for (int st = 0; st < 2; ++st) { q8[0][st] = row_part(sq, 2 * st); k8[0][st] = row_part(sk, 2 * st); }
-            }
-            if (kt + 1 < T::KT) {
-#pragma unroll
-              for (int st = 0; st < 2; ++st) {
-                q8[(kt + 1) & 1][st] = row_part(sq, 4 * (kt + 1) + 2 * st);
-                k8[(kt + 1) & 1][st] = row_part(sk, 4 * (kt + 1) + 2 * st);
-              }
-            }
-#pragma unroll
-            for (int st = 0; st < 2; ++st) {
-              P = linear_mfma(k8[kt & 1][st], q8[kt & 1][st], P);
-              float x[8];
-#pragma unroll
-              for (int i = 0; i < 8; ++i) x[i] = S[kt][8 * st + i];
-              const u32x4 s1 = linear_part(x), s2 = linear_last_part(x);
-              O = linear_mfma(s1, q8[kt & 1][st], O);
-              O = linear_mfma(s2, q8[kt & 1][st], O);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          P[e] *= wp[e];
-          O[e] *= wo;
-        }
-        if constexpr (F32) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) O = linear_mfma(column_float(sv, wave, e), P[e], O);
-        } else {
-#pragma unroll
-          for (int st = 0; st < 2; ++st) {
-            const u32x4 v8 = column_part(sv, wave, st);
-            float x[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = P[8 * st + i];
-            const u32x4 p1 = linear_part(x), p2 = linear_last_part(x);
-            O = linear_mfma(v8, p1, O);
-            O = linear_mfma(v8, p2, O);
-          }
-        }
-        if (l32 < m) {      // element e of O: token l32, column 32 wave + 8 (e / 4) + 4 half + e % 4
-          char* dst = a.out + (first + c0) * a.out_stride_b + (long long)(kvh * a.Gq + g) * T::SRCB + (unsigned)l32 * (unsigned)a.out_stride_b;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int col = 32 * wave + 8 * j + 4 * half;
-            const float x0 = O[4 * j] * a.scale, x1 = O[4 * j + 1] * a.scale, x2 = O[4 * j + 2] * a.scale, x3 = O[4 * j + 3] * a.scale;
-            if (F32) *(f32x4*)(dst + col * 4) = f32x4{x0, x1, x2, x3};
-            else *(u32x2*)(dst + col * 2) = u32x2{linear_pack(x0, x1), linear_pack(x2, x3)};
-          }
-        }
-      }
-      if (last_head) {      // the state goes past the chunk
-        float one = decay, lacks = 0.0f;      // (in place, and what is made good apart: two paths that end in other registers each cost a second state)
-        if (m < kLinearChunk) linear_decay(a.log_decay[kvh], m, one, lacks);
-        else if (++owed == 8) { lacks = 8.0f * rest; owed = 0; }
-#pragma unroll
-        for (int kt = 0; kt < T::KT; ++kt)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) S[kt][e] *= one;
-        if (lacks != 0.0f) {
-#pragma unroll
-          for (int kt = 0; kt < T::KT; ++kt)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) S[kt][e] = fmaf(S[kt][e], lacks, S[kt][e]);
-        }
-        advance(sk, sv);
-      }
-      // (into the buffers that were read a step ago: everyone is past that step's barrier)
-      qturn ^= 1;
-      if (last_head && !last_chunk) {
-        turn ^= 1;
-        put(rk, tiles[turn]);
-        put(rv, tiles[turn] + TILE);
-      }
-      if (OUT && !(last_head && last_chunk)) put(rq, tiles[qturn] + 2 * TILE);
+      if (OUT) outputs(c0, g, m, here, here + TILE, here + (OUT ? 2 * TILE : 0));
+      if (last_head) advance(m, here, here + TILE);
+      __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0): the next tiles are in LDS
       __syncthreads();
-    }
+      if (last_head && more && w.tokens - c1 < kLinearChunk) {      // the last chunk is short
+        weigh(w.tokens - c1);
+        __syncthreads();
+      }
+      c0 = c1;
+      g = g1;
+      return more;
+    };
+    stage(0, 0, tiles0);
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    __syncthreads();
+    bool more;      // (one way out: a second one costs a second state in registers)
+    do {
+      more = step(tiles0, tiles1);
+      if (more) more = step(tiles1, tiles0);
+    } while (more);
   }
   float* dst = !OUT ? linear_add(a, w, D) : !cut && to >= 0 ? a.states + to * a.state_stride : nullptr;
   if (dst != nullptr) {
-    const float owes = (float)owed * rest;
 #pragma unroll
     for (int kt = 0; kt < T::KT; ++kt) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) dst[state_at + (32 * kt + 8 * (e >> 2) + (e & 3)) * D] = fmaf(S[kt][e], owes, S[kt][e]);
+      for (int e = 0; e < 16; ++e) dst[state_at + (32 * kt + 8 * (e >> 2) + (e & 3)) * D] = S[kt][e] * f;
       __builtin_amdgcn_sched_barrier(0);
     }
   }
