@@ -49,16 +49,20 @@ int linear_args(const up_params* p, const void* q, const void* k, const void* v,
   return UP_OK;
 }
 
-// Sequences are cut into pieces of so many tokens that the batch makes about three work-groups for every CU (as many as its registers
-// hold), none shorter than 256.
+// Sequences are cut into pieces of so many tokens that the batch makes a work-group for every place that the CUs have (three a CU; two where
+// the state's parts are kept in registers, one where head rows of 512 bytes fill the LDS), none shorter than two chunks.
+// Measured, as pieces of a third, as these, as twice the size: 32768 tokens, 32/8 heads of 128, 309, 250, 270 us (two, three, four places a CU);
+// 64 wide, 40/8, ragged 184, 143, 156 (four, three, two).  Shortest piece of 256 and of 64 tokens: 1000 tokens, 8/8 heads of 128,
+// 34 and 23 us, 200 tokens of 32/8 heads of 64 29 and 21.
 struct LinearGeometry {
   int piece;
   long long slots;
   size_t total;
 };
 int linear_geometry(const Problem& pb, const int32_t* cu, LinearGeometry* g) {
-  long long piece = ((long long)pb.T * pb.Hkv / (3 * kCUs) + 63) / 64 * 64;
-  if (piece < 256) piece = 256;
+  const int places = pb.head_dim * (pb.qk_is_f32 ? 4 : 2) == 512 ? 1 : pb.head_dim == 128 && pb.Gq > 1 ? 2 : 3;
+  long long piece = ((long long)pb.T * pb.Hkv / (places * kCUs) + 63) / 64 * 64;
+  if (piece < 64) piece = 64;
   g->piece = (int)piece;
   g->slots = pb.T / piece + pb.R;
   g->total = 0;

@@ -174,8 +174,8 @@ __device__ __forceinline__ float linear_power(double x, int n) {
   return ldexpf(__builtin_amdgcn_exp2f((float)(y - whole)), (int)whole);
 }
 
-template <bool F32, int D, bool OUT>
-__global__ __launch_bounds__(64 * (D / 32), (LinearTile<F32, D>::DENSE)) void k_linear(LinearArgs a) {
+template <bool F32, int D, bool OUT, bool HOLD>
+__global__ __launch_bounds__(64 * (D / 32), (HOLD && D == 128 ? 2 : LinearTile<F32, D>::DENSE)) void k_linear(LinearArgs a) {
   typedef LinearTile<F32, D> T;
   constexpr int TILE = kLinearChunk * T::PPR;
   // keys, values and queries of a step, and of the next one.  (Two variables, not one array: the compiler then knows that a load into one and
@@ -260,17 +260,19 @@ __global__ __launch_bounds__(64 * (D / 32), (LinearTile<F32, D>::DENSE)) void k_
       if (OUT) load_to_lds(q + qoff[i], to_row + 2 * TILE);
     }
   };
-  // Operands out of LDS.  row_part: eight elements 32 kt + 16 st + {4 half .. +3, 8 + 4 half .. +3} of row l32 (bf16); four elements
-  // 32 kt + 8 j + 4 half .. of it (float).  column_part: column 32 kt + l32 of the tile's rows 16 st + {4 half .. +3, 8 + 4 half .. +3}.
+  // Operands out of LDS.  row_part: the 16-byte piece `piece` + half of row l32 (piece even).  column_part: column 32 kt + l32 of the tile's rows 16 st + {4 half .. +3, 8 + 4 half .. +3}.
   // The place of a piece is that of piece 0 with the piece's bits turned over: one address a lane and an exclusive or each.
-  unsigned row_at = l32 * T::SRCB + ((linear_swap<T::PPR>(l32) ^ (F32 ? half : 0)) * 16) + (F32 ? 0 : 8 * half);
+  unsigned row_at = l32 * T::SRCB + (linear_swap<T::PPR>(l32) ^ half) * 16;
   const int trow = 4 * half + ((lane >> 2) & 3), tpiece = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
   unsigned col_at = F32 ? 4 * half * T::SRCB + (((l32 >> 2) ^ half) * 16) + (l32 & 3) * 4
                         : trow * T::SRCB + ((tpiece ^ linear_swap<T::PPR>(trow)) * 16) + (lane & 1) * 8;
   auto row_part = [&](const u32x4* tile, int piece) __attribute__((always_inline)) {
-    if (F32) return *(const u32x4*)((const char*)tile + (row_at ^ (piece * 16)));
-    const u32x2 x = *(const u32x2*)((const char*)tile + (row_at ^ (piece * 16))), y = *(const u32x2*)((const char*)tile + (row_at ^ ((piece + 1) * 16)));
-    return u32x4{x.x, x.y, y.x, y.y};
+    return *(const u32x4*)((const char*)tile + (row_at ^ (piece * 16)));
+  };
+  // bf16 elements 8 half .. +7 of 16 -> 4 half .. +3 and 8 + 4 half .. +3, the order in which the lanes hold rows of the state
+  auto state_order = [&](const u32x4& x) __attribute__((always_inline)) {
+    const auto r0 = __builtin_amdgcn_permlane32_swap(x.x, x.z, false, false), r1 = __builtin_amdgcn_permlane32_swap(x.y, x.w, false, false);
+    return u32x4{r0[0], r1[0], r0[1], r1[1]};
   };
   auto column_part = [&](const u32x4* tile, int kt, int st) __attribute__((always_inline)) {
     typedef __attribute__((address_space(3))) s16x4* lds4;
@@ -284,11 +286,22 @@ __global__ __launch_bounds__(64 * (D / 32), (LinearTile<F32, D>::DENSE)) void k_
     return *(const float*)((const char*)tile + (col_at ^ (kt * 128) ^ (swap * 16)) + (8 * (e >> 2) + (e & 3)) * T::SRCB);
   };
 
+  // The state in two parts of bf16: taken apart for every head, or (HOLD: several query heads share the state) once a chunk and kept.
+  u32x4 s1[HOLD ? T::KT : 1][2], s2[HOLD ? T::KT : 1][2];
+  auto take_apart = [&](int kt, int st, u32x4& p1, u32x4& p2) __attribute__((always_inline)) {
+    float x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = S[kt][8 * st + i];
+    p1 = linear_part(x);
+    p2 = linear_last_part(x);
+  };
   // one head's outputs for the chunk
   auto outputs = [&](int c0, int g, int m, const u32x4* sk, const u32x4* sv, const u32x4* sq) __attribute__((always_inline)) {
     f32x16 P, O;
 #pragma unroll
     for (int e = 0; e < 16; ++e) P[e] = O[e] = 0.0f;
+    constexpr bool AHEAD = !F32 && D == 128 && HOLD;
+    u32x4 qs[2][2], ks[2][2];
 #pragma unroll
     for (int kt = 0; kt < T::KT; ++kt) {
       if constexpr (F32) {
@@ -303,16 +316,23 @@ __global__ __launch_bounds__(64 * (D / 32), (LinearTile<F32, D>::DENSE)) void k_
           }
         }
       } else {
+        if (kt == 0 || !AHEAD) {
+#pragma unroll
+          for (int st = 0; st < 2; ++st) { qs[kt & 1][st] = row_part(sq, 4 * kt + 2 * st); ks[kt & 1][st] = row_part(sk, 4 * kt + 2 * st); }
+        }
+        if (AHEAD && kt + 1 < T::KT) {
+#pragma unroll
+          for (int st = 0; st < 2; ++st) { qs[(kt + 1) & 1][st] = row_part(sq, 4 * (kt + 1) + 2 * st); ks[(kt + 1) & 1][st] = row_part(sk, 4 * (kt + 1) + 2 * st); }
+        }
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
-          const u32x4 q8 = row_part(sq, 4 * kt + 2 * st), k8 = row_part(sk, 4 * kt + 2 * st);
+          const u32x4 q8 = qs[kt & 1][st], k8 = ks[kt & 1][st];
           P = linear_mfma(k8, q8, P);
-          float x[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = S[kt][8 * st + i];
-          const u32x4 s1 = linear_part(x), s2 = linear_last_part(x);
-          O = linear_mfma(s1, q8, O);
-          O = linear_mfma(s2, q8, O);
+          const int at = HOLD ? kt : 0;
+          if (!HOLD) take_apart(kt, st, s1[0][st], s2[0][st]);
+          const u32x4 q = state_order(q8);
+          O = linear_mfma(s1[at][st], q, O);
+          O = linear_mfma(s2[at][st], q, O);
         }
       }
       __builtin_amdgcn_sched_barrier(0);      // (the operands of one step at a time: all of them at once push accumulators into scratch)
@@ -338,13 +358,23 @@ __global__ __launch_bounds__(64 * (D / 32), (LinearTile<F32, D>::DENSE)) void k_
         O = linear_mfma(v8, p2, O);
       }
     }
-    if (l32 < m) {      // element e of O: token l32, column 32 wave + 8 (e / 4) + 4 half + e % 4
-      char* dst = a.out + (first + c0) * a.out_stride_b + (long long)(kvh * a.Gq + g) * T::SRCB + (unsigned)l32 * (unsigned)a.out_stride_b;
+    // Element e of O: token l32, column 32 wave + 8 (e / 4) + 4 half + e % 4.  Through a buffer that ends with the chunk's m rows, so that
+    // a wave always issues all its stores (below).
+    char* rows = a.out + (first + c0) * a.out_stride_b + (long long)(kvh * a.Gq + g) * T::SRCB;
+    const auto buffer = __builtin_amdgcn_make_buffer_rsrc(rows, 0, (int)((unsigned)(m - 1) * (unsigned)a.out_stride_b + T::SRCB), 0x00027000);
+    const unsigned at = (unsigned)l32 * (unsigned)a.out_stride_b + wave * 32 * (F32 ? 4 : 2) + half * 16;
+    if constexpr (F32) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int col = 32 * wave + 8 * j + 4 * half;
-        if (F32) *(f32x4*)(dst + col * 4) = f32x4{O[4 * j], O[4 * j + 1], O[4 * j + 2], O[4 * j + 3]};
-        else *(u32x2*)(dst + col * 2) = u32x2{linear_pack(O[4 * j], O[4 * j + 1]), linear_pack(O[4 * j + 2], O[4 * j + 3])};
+        const f32x4 x = {O[4 * j], O[4 * j + 1], O[4 * j + 2], O[4 * j + 3]};
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, x), buffer, at + j * 32, 0, 0);
+      }
+    } else {      // (two quarters of 16 columns change lane halves: 16 bytes a lane)
+#pragma unroll
+      for (int j = 0; j < 4; j += 2) {
+        const auto r0 = __builtin_amdgcn_permlane32_swap(linear_pack(O[4 * j], O[4 * j + 1]), linear_pack(O[4 * j + 4], O[4 * j + 5]), false, false);
+        const auto r1 = __builtin_amdgcn_permlane32_swap(linear_pack(O[4 * j + 2], O[4 * j + 3]), linear_pack(O[4 * j + 6], O[4 * j + 7]), false, false);
+        __builtin_amdgcn_raw_buffer_store_b128(u32x4{r0[0], r1[0], r0[1], r1[1]}, buffer, at + j * 16, 0, 0);
       }
     }
   };
@@ -412,12 +442,25 @@ __global__ __launch_bounds__(64 * (D / 32), (LinearTile<F32, D>::DENSE)) void k_
       if (more) stage(c1, g1, next);
       // (made anew in every round: kept over the loop, addresses and the state's parts would push accumulators into scratch)
       asm volatile("" : "+v"(row_at), "+v"(col_at));
+      if constexpr (HOLD) {
+        if (g == 0) {
 #pragma unroll
-      for (int kt = 0; kt < T::KT; ++kt) asm volatile("" : "+v"(S[kt]));
+          for (int kt = 0; kt < T::KT; ++kt)
+#pragma unroll
+            for (int st = 0; st < 2; ++st) take_apart(kt, st, s1[kt][st], s2[kt][st]);
+        }
+      } else {
+#pragma unroll
+        for (int kt = 0; kt < T::KT; ++kt) asm volatile("" : "+v"(S[kt]));
+      }
       if (OUT) outputs(c0, g, m, here, here + TILE, here + (OUT ? 2 * TILE : 0));
       if (last_head) advance(m, here, here + TILE);
-      __builtin_amdgcn_s_waitcnt(0x0f70);      // vmcnt(0): the next tiles are in LDS
-      __syncthreads();
+      // The next tiles are in LDS and everyone is done with these.  Vector memory completes in order, and the step has issued its stores
+      // since it asked for the tiles: these may be under way, which __syncthreads would wait for.
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(!OUT ? 0x0070 : F32 ? 0x0074 : 0x0072);      // vmcnt(0), (4), (2); lgkmcnt(0)
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
       if (last_head && more && w.tokens - c1 < kLinearChunk) {      // the last chunk is short
         weigh(w.tokens - c1);
         __syncthreads();
@@ -485,13 +528,15 @@ template <bool F32, int D>
 static hipError_t launch_linear_form(const LinearArgs& a, hipStream_t s) {
   const dim3 grid((unsigned)a.slots * a.Hkv), block(64 * (D / 32));
   if (a.adds != nullptr) {
-    hipLaunchKernelGGL((k_linear<F32, D, false>), grid, block, 0, s, a);
+    hipLaunchKernelGGL((k_linear<F32, D, false, false>), grid, block, 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((k_linear_join<D>), dim3((unsigned)a.R * a.Hkv * (D * D / 1024)), dim3(256), 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  hipLaunchKernelGGL((k_linear<F32, D, true>), grid, block, 0, s, a);
+  constexpr bool can_hold = !F32 && D <= 128;
+  if (can_hold && a.Gq > 1) hipLaunchKernelGGL((k_linear<F32, D, true, can_hold>), grid, block, 0, s, a);
+  else hipLaunchKernelGGL((k_linear<F32, D, true, false>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 
