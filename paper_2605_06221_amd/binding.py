@@ -155,6 +155,17 @@ def ptr(x):
     return ctypes.c_void_p(x.data_ptr())      # torch tensor
 
 
+def _addr(x):
+    """ptr without the c_void_p object, which the declared argument types do not need: 0.2 instead of 0.4 us an argument, and the calls
+    of a decode step have fifteen."""
+    if x is None:
+        return None
+    try:
+        return x.data_ptr()
+    except AttributeError:
+        return x if isinstance(x, int) else x.ctypes.data
+
+
 def _stream(stream):
     if stream is None:
         import torch
@@ -532,7 +543,7 @@ def uniprefill_cache_evict(k_cache, v_cache, row_bytes, cache_row_stride, mass, 
 def uniprefill_attention_window_plan(p: up_params, cu_seqlens_host: np.ndarray, cu_seqlens_k_host, window, n_sink, *, check: bool = True):
     """Returns (status, workspace_bytes)."""
     ws = ctypes.c_size_t(0)
-    st = _lib.uniprefill_attention_window_plan(ctypes.byref(p), ptr(cu_seqlens_host), ptr(cu_seqlens_k_host), int(window), int(n_sink),
+    st = _lib.uniprefill_attention_window_plan(ctypes.byref(p), _addr(cu_seqlens_host), _addr(cu_seqlens_k_host), int(window), int(n_sink),
                                                ctypes.byref(ws))
     _check(st, "uniprefill_attention_window_plan", check)
     return st, int(ws.value)
@@ -541,10 +552,10 @@ def uniprefill_attention_window_plan(p: up_params, cu_seqlens_host: np.ndarray, 
 def uniprefill_attention_window(p, q, k, v, v_row_stride, cu_seqlens_dev, cu_seqlens_host, cu_seqlens_k_dev, cu_seqlens_k_host,
                                 block_table, block_table_stride, kv_block_size, window, n_sink, out, out_row_stride, lse_out,
                                 lse_row_stride, workspace, workspace_bytes, stream=None, check=True):
-    st = _lib.uniprefill_attention_window(ctypes.byref(p), ptr(q), ptr(k), ptr(v), int(v_row_stride), ptr(cu_seqlens_dev),
-                                          ptr(cu_seqlens_host), ptr(cu_seqlens_k_dev), ptr(cu_seqlens_k_host), ptr(block_table),
-                                          int(block_table_stride), int(kv_block_size), int(window), int(n_sink), ptr(out),
-                                          int(out_row_stride), ptr(lse_out), int(lse_row_stride), ptr(workspace), workspace_bytes,
+    st = _lib.uniprefill_attention_window(ctypes.byref(p), _addr(q), _addr(k), _addr(v), int(v_row_stride), _addr(cu_seqlens_dev),
+                                          _addr(cu_seqlens_host), _addr(cu_seqlens_k_dev), _addr(cu_seqlens_k_host), _addr(block_table),
+                                          int(block_table_stride), int(kv_block_size), int(window), int(n_sink), _addr(out),
+                                          int(out_row_stride), _addr(lse_out), int(lse_row_stride), _addr(workspace), workspace_bytes,
                                           _stream(stream))
     return _check(st, "uniprefill_attention_window", check)
 
@@ -560,34 +571,34 @@ def uniprefill_attention_window_step_plan(p: up_params, max_kv_len, window, n_si
 def uniprefill_attention_window_step(p, q, k_cache, v_cache, v_row_stride, kv_len_dev, max_kv_len, block_table, block_table_stride,
                                      kv_block_size, window, n_sink, out, out_row_stride, lse_out, lse_row_stride, workspace,
                                      workspace_bytes, stream=None, check=True):
-    st = _lib.uniprefill_attention_window_step(ctypes.byref(p), ptr(q), ptr(k_cache), ptr(v_cache), int(v_row_stride),
-                                               ptr(kv_len_dev), int(max_kv_len), ptr(block_table), int(block_table_stride),
-                                               int(kv_block_size), int(window), int(n_sink), ptr(out), int(out_row_stride),
-                                               ptr(lse_out), int(lse_row_stride), ptr(workspace), workspace_bytes, _stream(stream))
+    st = _lib.uniprefill_attention_window_step(ctypes.byref(p), _addr(q), _addr(k_cache), _addr(v_cache), int(v_row_stride),
+                                               _addr(kv_len_dev), int(max_kv_len), _addr(block_table), int(block_table_stride),
+                                               int(kv_block_size), int(window), int(n_sink), _addr(out), int(out_row_stride),
+                                               _addr(lse_out), int(lse_row_stride), _addr(workspace), workspace_bytes, _stream(stream))
     return _check(st, "uniprefill_attention_window_step", check)
 
 
 def uniprefill_linear_attention_plan(p: up_params, cu_seqlens_host: np.ndarray, *, check: bool = True):
     """Returns (status, workspace_bytes)."""
     ws = ctypes.c_size_t(0)
-    st = _lib.uniprefill_linear_attention_plan(ctypes.byref(p), ptr(cu_seqlens_host), ctypes.byref(ws))
+    st = _lib.uniprefill_linear_attention_plan(ctypes.byref(p), _addr(cu_seqlens_host), ctypes.byref(ws))
     _check(st, "uniprefill_linear_attention_plan", check)
     return st, int(ws.value)
 
 
 def uniprefill_linear_attention(p, q, k, v, v_row_stride, cu_seqlens_dev, cu_seqlens_host, log_decay, states, state_stride, num_states,
                                 state_in, state_out, out, out_row_stride, workspace, workspace_bytes, stream=None, check=True):
-    st = _lib.uniprefill_linear_attention(ctypes.byref(p), ptr(q), ptr(k), ptr(v), int(v_row_stride), ptr(cu_seqlens_dev),
-                                          ptr(cu_seqlens_host), ptr(log_decay), ptr(states), int(state_stride), int(num_states),
-                                          ptr(state_in), ptr(state_out), ptr(out), int(out_row_stride), ptr(workspace),
+    st = _lib.uniprefill_linear_attention(ctypes.byref(p), _addr(q), _addr(k), _addr(v), int(v_row_stride), _addr(cu_seqlens_dev),
+                                          _addr(cu_seqlens_host), _addr(log_decay), _addr(states), int(state_stride), int(num_states),
+                                          _addr(state_in), _addr(state_out), _addr(out), int(out_row_stride), _addr(workspace),
                                           workspace_bytes, _stream(stream))
     return _check(st, "uniprefill_linear_attention", check)
 
 
 def uniprefill_linear_attention_step(p, q, k, v, v_row_stride, log_decay, states, state_stride, num_states, state_in, state_out, out,
                                      out_row_stride, stream=None, check=True):
-    st = _lib.uniprefill_linear_attention_step(ctypes.byref(p), ptr(q), ptr(k), ptr(v), int(v_row_stride), ptr(log_decay), ptr(states),
-                                               int(state_stride), int(num_states), ptr(state_in), ptr(state_out), ptr(out),
+    st = _lib.uniprefill_linear_attention_step(ctypes.byref(p), _addr(q), _addr(k), _addr(v), int(v_row_stride), _addr(log_decay), _addr(states),
+                                               int(state_stride), int(num_states), _addr(state_in), _addr(state_out), _addr(out),
                                                int(out_row_stride), _stream(stream))
     return _check(st, "uniprefill_linear_attention_step", check)
 
@@ -595,18 +606,18 @@ def uniprefill_linear_attention_step(p, q, k, v, v_row_stride, log_decay, states
 def uniprefill_norm_rotate(p, q, k, v, v_row_stride, q_weight, k_weight, eps, pos, inv_freq, rot_dim, pairs, count_dev, q_out,
                            q_out_row_stride, k_out, k_out_row_stride, v_out, v_out_row_stride, slots, num_slots, stream=None,
                            check=True):
-    st = _lib.uniprefill_norm_rotate(ctypes.byref(p), ptr(q), ptr(k), ptr(v), int(v_row_stride), ptr(q_weight), ptr(k_weight),
-                                     float(eps), ptr(pos), ptr(inv_freq), int(rot_dim), int(pairs), ptr(count_dev), ptr(q_out),
-                                     int(q_out_row_stride), ptr(k_out), int(k_out_row_stride), ptr(v_out), int(v_out_row_stride),
-                                     ptr(slots), int(num_slots), _stream(stream))
+    st = _lib.uniprefill_norm_rotate(ctypes.byref(p), _addr(q), _addr(k), _addr(v), int(v_row_stride), _addr(q_weight), _addr(k_weight),
+                                     float(eps), _addr(pos), _addr(inv_freq), int(rot_dim), int(pairs), _addr(count_dev), _addr(q_out),
+                                     int(q_out_row_stride), _addr(k_out), int(k_out_row_stride), _addr(v_out), int(v_out_row_stride),
+                                     _addr(slots), int(num_slots), _stream(stream))
     return _check(st, "uniprefill_norm_rotate", check)
 
 
 def uniprefill_append_pages(kv_len_dev, num_new_dev, num_seqs, kv_block_size, block_table, block_table_stride, free_pages,
                             num_free_dev, free_left_dev, new_len_dev, cu_seqlens_dev, cu_seqlens_k_dev, pos, slots, capacity,
                             num_served_dev, stream=None, check=True):
-    st = _lib.uniprefill_append_pages(ptr(kv_len_dev), ptr(num_new_dev), int(num_seqs), int(kv_block_size), ptr(block_table),
-                                      int(block_table_stride), ptr(free_pages), ptr(num_free_dev), ptr(free_left_dev),
-                                      ptr(new_len_dev), ptr(cu_seqlens_dev), ptr(cu_seqlens_k_dev), ptr(pos), ptr(slots),
-                                      int(capacity), ptr(num_served_dev), _stream(stream))
+    st = _lib.uniprefill_append_pages(_addr(kv_len_dev), _addr(num_new_dev), int(num_seqs), int(kv_block_size), _addr(block_table),
+                                      int(block_table_stride), _addr(free_pages), _addr(num_free_dev), _addr(free_left_dev),
+                                      _addr(new_len_dev), _addr(cu_seqlens_dev), _addr(cu_seqlens_k_dev), _addr(pos), _addr(slots),
+                                      int(capacity), _addr(num_served_dev), _stream(stream))
     return _check(st, "uniprefill_append_pages", check)

@@ -129,7 +129,7 @@ int attn_step_geometry(const Problem& pb, int max_len, const AttnWindow& w, Attn
   g->reach = (int)(reach < max_len ? reach : max_len);
   const long long groups = (long long)pb.R * pb.Hkv, want = groups > 0 ? (2 * kCUs + groups - 1) / groups : 1;
   long long part = ((g->reach + want - 1) / want + 127) / 128 * 128;
-  if (part < 512) part = 512;
+  if (part < 128) part = 128;
   g->parts = imax(1, attn_pieces(g->reach, (int)part));
   g->slots = pb.R;
   g->items = (long long)pb.R * g->parts;

@@ -62,6 +62,8 @@ struct PagesArgs {
   int32_t* served;
   long long capacity;
   int R, kv_block;
+  unsigned kv_magic;               // 0xFFFFFFFF / kv_block
+  int one_launch;
 };
 
 #if defined(__HIPCC__)

@@ -270,6 +270,7 @@ int uniprefill_append_pages(const int32_t* kv_len_dev, const int32_t* num_new_de
   a.block_table = block_table; a.table_stride = block_table_stride; a.free_left = free_left_dev; a.new_len = new_len_dev;
   a.cu = cu_seqlens_dev; a.cu_k = cu_seqlens_k_dev; a.pos = pos; a.slots = slots; a.served = num_served_dev;
   a.capacity = capacity; a.R = num_seqs; a.kv_block = kv_block_size;
+  a.kv_magic = 0xFFFFFFFFu / (unsigned)kv_block_size;
   return launch_pages(a, (hipStream_t)stream) == hipSuccess ? UP_OK : UP_ERR_HIP;
 }
 

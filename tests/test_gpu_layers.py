@@ -596,7 +596,7 @@ def _requests(seed, n, most):
 
 
 @pytest.mark.parametrize("page", [1, 7, 16, 128])
-@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 1023, 1024, 1025, 2500])
+@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 1023, 1024, 1025, 2500, 4095, 4096, 4097, 9000])
 def test_pages(n, page):
     _say("pages", n, page)
     lengths, new = _requests(n + page, n, 130)
