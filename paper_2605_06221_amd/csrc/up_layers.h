@@ -43,6 +43,7 @@ struct RotateArgs {
   int D, rot;
   int pairs;
   int waves;                       // waves that share a token
+  int stream;                      // more bytes than the last-level cache holds
 };
 
 // --- pages for new tokens
