@@ -547,6 +547,24 @@ def test_rotation_at_far_positions_and_of_zero_rows():
     b.check()
 
 
+def test_rotation_past_the_cache_gives_the_same_bits():
+    _say("rotate: more bytes than the cache holds, against the same rows in parts")
+    n, hq, hkv, D = 12001, 40, 8, 128
+    b = Rotate(6, n, hq, hkv, D)
+    assert 2 * n * (hq + 2 * hkv) * D * 2 > 256 << 20
+    b.run()
+    q, k, v = b.views()
+    want_q, want_k, want_v = (torch.full_like(t, -7.0) for t in (b.q_out, b.k_out, b.v_out))
+    for lo in range(0, n, 3000):
+        hi = min(n, lo + 3000)
+        p = up.make_params(num_seqs=1, total_tokens=hi - lo, block_size=64, num_q_heads=hq, num_kv_heads=hkv, head_dim=D, q_row_stride=b.row,
+                           k_row_stride=b.row)
+        up.uniprefill_norm_rotate(p, q[lo:], k[lo:], v[lo:], b.row, b.w[0], b.w[1], b.eps, b.pos[lo:hi].clone(), b.freq, b.rot, 0, None, want_q[lo:],
+                                  hq * D, want_k, hkv * D, want_v, hkv * D, b.slots[lo:hi].clone(), b.num)
+    for got, want in ((b.q_out, want_q), (b.k_out, want_k), (b.v_out, want_v)):
+        assert torch.equal(got, want)
+
+
 # ---------------------------------------------------------------------------------------------------- pages
 class Pages:
     def __init__(self, seed, lengths, new, page, spare=3, slack=2, capacity=None):
@@ -639,3 +657,142 @@ def test_pages_step_by_step_in_a_graph():
         want = b.check(in_place=True)
         b.len_host, b.num_free, b.table_host = np.asarray(want["new_len"], np.int32), want["free_left"], want["table"].astype(np.int32)
     assert want["served"] < 5
+
+
+# ---------------------------------------------------------------------------------------------------- all of them in a row
+def test_the_layers_of_a_hybrid_model_in_a_row():
+    """Two requests, one of them new, the other with cached context: pages for their tokens, norm and rotation into the cache, windowed
+    attention over it, linear attention of the same rows from and to states; then a drop of tokens and the layers behind it on what is left;
+    then three decode steps, captured once and replayed.  Every stage against the oracle on what the stage before left."""
+    _say("pages, rotation, windowed and linear attention, a drop, decode steps")
+    rng = np.random.default_rng(77)
+    hq, hkv, D, page, window, n_sink = 8, 2, 128, 16, 40, 4
+    u = 2.0 ** -8
+    had, new = [37, 0], [150, 93]
+    R, T, most, pool = 2, sum(new), 20, 64
+    table_host = np.full((R, most), -1, np.int32)
+    order = rng.permutation(pool).astype(np.int32)
+    table_host[0, :3] = order[:3]
+    free_host = order[3:]
+    table, free = _dev(table_host), _dev(free_host)
+    num_free, kv_len = torch.tensor([len(free_host)], dtype=torch.int32, device="cuda"), torch.tensor(had, dtype=torch.int32, device="cuda")
+    cu, cu_k, served = (torch.zeros(n, dtype=torch.int32, device="cuda") for n in (R + 1, R + 1, 1))
+    pos, slots = torch.zeros(T, dtype=torch.int32, device="cuda"), torch.zeros(T, dtype=torch.int64, device="cuda")
+    k_cache, _ = _rows(rng, BF, pool * page, hkv, D)
+    v_cache, _ = _rows(rng, BF, pool * page, hkv, D)
+    k_cache, v_cache = k_cache.cuda().reshape(-1, hkv * D), v_cache.cuda().reshape(-1, hkv * D)
+    states = torch.from_numpy(rng.standard_normal((2, hkv, D, D)).astype(np.float32)).cuda()
+    ld = np.array([-0.2, -0.01], np.float32)
+    log_decay, state_slot = _dev(ld), _dev(np.array([1, 0], np.int32))
+    state_from = _dev(np.array([1, -1], np.int32))
+    freq = (10000.0 ** (-np.arange(0, D, 2) / D)).astype(np.float32)
+    w, w64 = _rows(rng, BF, 2, D)
+    w, freq_dev = w.cuda(), _dev(freq)
+
+    def ints(x):
+        return x.cpu().numpy()
+
+    def params(tokens, seqs=R):
+        return up.make_params(num_seqs=seqs, total_tokens=tokens, block_size=64, num_q_heads=hq, num_kv_heads=hkv, head_dim=D)
+
+    def host(x, heads):
+        return x.double().cpu().numpy().reshape(-1, heads, D)
+
+    # ---- a prompt and a chunk
+    want = lo.append_pages(had, new, page, table_host, free_host, len(free_host), T)
+    up.uniprefill_append_pages(kv_len, _dev(np.array(new, np.int32)), R, page, table, most, free, num_free, num_free, kv_len, cu, cu_k, pos, slots, T, served)
+    for name, got in (("table", table), ("new_len", kv_len), ("cu", cu), ("cu_k", cu_k), ("pos", pos), ("slots", slots)):
+        np.testing.assert_array_equal(ints(got), np.asarray(want[name]), err_msg=name)
+    q, q64 = _rows(rng, BF, T, hq, D)
+    k, k64 = _rows(rng, BF, T, hkv, D)
+    v, v64 = _rows(rng, BF, T, hkv, D)
+    q, k, v = (t.cuda() for t in (q, k, v))
+    q_out = torch.empty_like(q)
+    p = params(T)
+    up.uniprefill_norm_rotate(p, q, k, v, hkv * D, w[0], w[1], 1e-6, pos, freq_dev, D, 0, None, q_out, hq * D, k_cache, hkv * D, v_cache, hkv * D, slots, pool * page)
+    ref, size = lo.norm_rotate(q64, w64[0], 1e-6, want["pos"], freq, D, False)
+    assert (np.abs(host(q_out, hq) - ref) <= u * np.abs(ref) + (D + 40) * F * size).all()
+    ref, size = lo.norm_rotate(k64, w64[1], 1e-6, want["pos"], freq, D, False)
+    assert (np.abs(host(k_cache, hkv)[want["slots"]] - ref) <= u * np.abs(ref) + (D + 40) * F * size).all()
+    assert torch.equal(v_cache[slots], v.reshape(T, -1))
+    cu_host, ck_host = np.asarray(want["cu"], np.int32), np.asarray(want["cu_k"], np.int32)
+    _, nb = up.uniprefill_attention_window_plan(p, cu_host, ck_host, window, n_sink)
+    ws = torch.empty(nb + 256, dtype=torch.uint8, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty(hq, T, device="cuda")
+    up.uniprefill_attention_window(p, q_out, k_cache, v_cache, hkv * D, cu, cu_host, cu_k, ck_host, table, most, page, window, n_sink, out, hq * D, lse, T, ws, nb)
+    gather = lambda r, n: ao.page_rows(want["table"][r].astype(np.int32), n, page)
+    o, z, absv, top = lo.window_attention(host(q_out, hq), host(k_cache, hkv), host(v_cache, hkv), cu_host, ck_host, window, n_sink, gather=gather)
+    assert (np.abs(host(out, hq) - o) <= _attention_tolerance(o, absv, top, max(want["new_len"]), D, True)).all()
+    assert (np.abs(lse.double().cpu().numpy() - z) <= _lse_tolerance(z, top, max(want["new_len"]), D)).all()
+
+    def linear(tokens, q, k, v, cu, cu_host, start):
+        before = states.double().cpu().numpy()
+        p = params(tokens)
+        _, nb = up.uniprefill_linear_attention_plan(p, cu_host)
+        ws = torch.empty(nb + 256, dtype=torch.uint8, device="cuda")
+        y = torch.empty_like(q)
+        up.uniprefill_linear_attention(p, q, k, v, hkv * D, cu, cu_host, log_decay, states, hkv * D * D, 2, start, state_slot, y, hq * D, ws, nb)
+        o, pool, bound, pbound = lo.linear_attention(host(q, hq), host(k, hkv), host(v, hkv), cu_host, ld, before, ints(start), ints(state_slot))
+        n = int(np.diff(cu_host).max())
+        assert (np.abs(host(y, hq) - o) <= u * np.abs(o) + ((3 * n + D + 512) * F + 2.0 ** -15) * bound).all()
+        assert (np.abs(states.double().cpu().numpy() - pool) <= (3 * n + 512) * F * pbound).all()
+    linear(T, q, k, v, cu, cu_host, state_from)
+
+    # ---- a drop, and the layers behind it on the tokens that stay
+    keep = np.sort(rng.permutation(T)[:101]).astype(np.int32)
+    kept_cu_host = np.searchsorted(keep, cu_host).astype(np.int32)
+    kept, kept_cu, n = _dev(keep), _dev(kept_cu_host), len(keep)
+    q2, k2, v2 = (t[kept.long()].contiguous() for t in (q, k, v))
+    pos2 = torch.empty(n, dtype=torch.int32, device="cuda")
+    up.uniprefill_compact_column(pos, 4, kept, n, None, pos2)
+    k2_out, v2_out, q2_out = torch.empty_like(k2), torch.empty_like(v2), torch.empty_like(q2)
+    p2 = params(n)
+    up.uniprefill_norm_rotate(p2, q2, k2, v2, hkv * D, None, None, 1e-6, pos2, freq_dev, D, 0, None, q2_out, hq * D, k2_out, hkv * D, v2_out, hkv * D, None, 0)
+    ref, size = lo.norm_rotate(host(k2, hkv), None, 1e-6, np.asarray(want["pos"])[keep], freq, D, False)
+    assert (np.abs(host(k2_out, hkv) - ref) <= u * np.abs(ref) + (D + 40) * F * size).all()
+    _, nb = up.uniprefill_attention_window_plan(p2, kept_cu_host, None, window, n_sink)
+    ws = torch.empty(nb + 256, dtype=torch.uint8, device="cuda")
+    out2 = torch.empty_like(q2)
+    up.uniprefill_attention_window(p2, q2_out, k2_out, v2_out, hkv * D, kept_cu, kept_cu_host, None, None, None, 0, page, window, n_sink, out2, hq * D, None, 0, ws, nb)
+    o, _, absv, top = lo.window_attention(host(q2_out, hq), host(k2_out, hkv), host(v2_out, hkv), kept_cu_host, kept_cu_host, window, n_sink)
+    assert (np.abs(host(out2, hq) - o) <= _attention_tolerance(o, absv, top, n, D, True)).all()
+    linear(n, q2, k2, v2, kept_cu, kept_cu_host, state_slot)
+
+    # ---- decode steps of both, from a graph
+    p3 = params(R)
+    one = torch.ones(R, dtype=torch.int32, device="cuda")
+    q3, k3, v3 = (torch.zeros(R, h * D, dtype=BF, device="cuda") for h in (hq, hkv, hkv))
+    q3_out, out3, y3 = torch.zeros_like(q3), torch.zeros_like(q3), torch.zeros_like(q3)
+    lse3 = torch.zeros(hq, R, device="cuda")
+    _, nb3 = up.uniprefill_attention_window_step_plan(p3, most * page, window, n_sink)
+    ws3 = torch.empty(nb3 + 256, dtype=torch.uint8, device="cuda")
+    pos3, slots3 = torch.zeros(R, dtype=torch.int32, device="cuda"), torch.zeros(R, dtype=torch.int64, device="cuda")
+
+    def step():
+        up.uniprefill_append_pages(kv_len, one, R, page, table, most, free, num_free, num_free, kv_len, cu, cu_k, pos3, slots3, R, served)
+        up.uniprefill_norm_rotate(p3, q3, k3, v3, hkv * D, w[0], w[1], 1e-6, pos3, freq_dev, D, 0, None, q3_out, hq * D, k_cache, hkv * D, v_cache, hkv * D, slots3, pool * page)
+        up.uniprefill_attention_window_step(p3, q3_out, k_cache, v_cache, hkv * D, kv_len, most * page, table, most, page, window, n_sink, out3, hq * D, lse3, R, ws3, nb3)
+        up.uniprefill_linear_attention_step(p3, q3, k3, v3, hkv * D, log_decay, states, hkv * D * D, 2, state_slot, state_slot, y3, hq * D)
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        step()
+    lengths, table_now, left = want["new_len"], want["table"], want["free_left"]
+    for _ in range(20):
+        for t in (q3, k3, v3):
+            t.copy_(_rows(rng, BF, *t.shape)[0])
+        before = states.double().cpu().numpy()
+        g.replay()
+        want = lo.append_pages(lengths, [1, 1], page, table_now, free_host, left, R)
+        lengths, table_now, left = want["new_len"], want["table"], want["free_left"]
+        np.testing.assert_array_equal(ints(table), table_now)
+        np.testing.assert_array_equal(ints(slots3), want["slots"])
+        ref, size = lo.norm_rotate(host(q3, hq), w64[0], 1e-6, want["pos"], freq, D, False)
+        assert (np.abs(host(q3_out, hq) - ref) <= u * np.abs(ref) + (D + 40) * F * size).all()
+        gather = lambda r, n: ao.page_rows(table_now[r].astype(np.int32), n, page)
+        o, z, absv, top = lo.window_attention(host(q3_out, hq), host(k_cache, hkv), host(v_cache, hkv), _cu([1, 1]), _cu(lengths), window, n_sink, gather=gather)
+        assert (np.abs(host(out3, hq) - o) <= _attention_tolerance(o, absv, top, max(lengths), D, True)).all()
+        assert (np.abs(lse3.double().cpu().numpy() - z) <= _lse_tolerance(z, top, max(lengths), D)).all()
+        o, pool_now, bound, pbound = lo.linear_attention(host(q3, hq), host(k3, hkv), host(v3, hkv), _cu([1, 1]), ld, before, [1, 0], [1, 0])
+        assert (np.abs(host(y3, hq) - o) <= u * np.abs(o) + (D + 515) * F * bound).all()
+        assert (np.abs(states.double().cpu().numpy() - pool_now) <= 515 * F * pbound).all()
