@@ -682,7 +682,7 @@ int uniprefill_attention_window_step(const up_params* p, const void* q, const vo
  *   out          as for uniprefill_attention; overlaps none of q, k, v
  *   workspace    from uniprefill_linear_attention_plan with the same lengths
  *                (256-byte aligned; 0 bytes, and NULL, where no sequence is cut)
- * Refusals as for uniprefill_attention; rows (of q and out too) more than 2^27 bytes apart, and
+ * Refusals as for uniprefill_attention; more than 2^30 tokens, rows (of q and out too) more than 2^27 bytes apart, and
  * more than (2^32 - 1) / 256 work-groups (num_seqs * num_kv_heads * (head_dim / 32)^2 of them at most):
  * UP_ERR_UNSUPPORTED. */
 int uniprefill_linear_attention_plan(const up_params* p, const int32_t* cu_seqlens_host, size_t* workspace_bytes);
@@ -744,7 +744,7 @@ int uniprefill_norm_rotate(const up_params* p, const void* q, const void* k, con
  *   pos, slots       [capacity] int32 position and int64 slot of every token served, in order; the rest
  *                    is filled with 0 and -1, the slot that the cache's entry points leave out
  *   num_served_dev   [1] sequences served
- * Lengths beyond what a row of the table holds are not served; entries of the table up to a sequence's
+ * The arrays overlap in no other way.  Lengths beyond what a row of the table holds are not served; entries of the table up to a sequence's
  * length must name its pages.  capacity and num_seqs up to 2^31 - 65537 (UP_ERR_UNSUPPORTED),
  * kv_block_size >= 1 and block_table_stride >= 0 (UP_ERR_RANGE). */
 int uniprefill_append_pages(const int32_t* kv_len_dev, const int32_t* num_new_dev, int32_t num_seqs,

@@ -60,6 +60,7 @@ struct LinearGeometry {
   size_t total;
 };
 int linear_geometry(const Problem& pb, const int32_t* cu, LinearGeometry* g) {
+  if (pb.T > 1 << 30) return UP_ERR_UNSUPPORTED;      // (a piece past the end of the last sequence is still counted in 31 bits)
   const int places = pb.head_dim * (pb.qk_is_f32 ? 4 : 2) == 512 ? 1 : pb.head_dim == 128 && pb.Gq > 1 ? 2 : 3;
   long long piece = ((long long)pb.T * pb.Hkv / (places * kCUs) + 63) / 64 * 64;
   if (piece < 64) piece = 64;

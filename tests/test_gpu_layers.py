@@ -119,6 +119,9 @@ def test_window_attention_with_the_keys_cut_into_pieces(lengths, earlier, hq, hk
     ([2100, 1, 67], None, 32, 8, 128, BF, 0, 700, 4), ([1100], [333], 64, 8, 64, BF, 16, 150, 128), ([700, 0, 400], [50, 0, 0], 64, 8, 256, BF, 8, 99, 33),
     ([1010], [129], 64, 16, 128, F32, 24, 400, 1), ([520, 1, 67], None, 256, 16, 64, BF, 0, 64, 0), ([2100, 1], [0, 9000], 32, 8, 128, BF, 16, 1000, 16),
     ([300], [700], 512, 8, 128, BF, 16, 600, 200), ([515], None, 256, 16, 64, F32, 7, 300, 0),
+    # windows wide enough for 256 rows whatever the width of the heads
+    ([1100], [3000], 64, 8, 64, BF, 16, 2500, 70), ([1100, 40], [2900, 0], 64, 8, 128, BF, 0, 2300, 200), ([1040], [2600], 64, 8, 64, F32, 7, 2100, 1),
+    ([1100], [2600], 64, 8, 128, BF, 24, 2222, 0),
 ])
 def test_window_attention_in_work_groups_of_256_rows(lengths, earlier, hq, hkv, D, dtype, page, window, n_sink):
     _say("window attention, large", lengths, earlier, hq, hkv, D, dtype, page, window, n_sink)

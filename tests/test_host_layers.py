@@ -147,6 +147,8 @@ def test_linear_refusals(kw, want):
     assert _linear(cu=None) == up.UP_ERR_NULL and _linear(cu_host=None) == up.UP_ERR_NULL
     assert _linear(cu_host=np.array([0, 60, 99], np.int32)) == up.UP_ERR_SHAPE
     assert _state(_params()) == up.UP_ERR_SHAPE
+    cu = np.array([0, 2 ** 30 + 1], np.int32)
+    assert up.uniprefill_linear_attention_plan(_params(num_seqs=1, total_tokens=2 ** 30 + 1), cu, check=False)[0] == up.UP_ERR_UNSUPPORTED
     n = 1 << 23
     assert _state(_params(num_seqs=n, total_tokens=n)) == up.UP_ERR_UNSUPPORTED
 
@@ -190,3 +192,19 @@ def _pages(**kw):
 ])
 def test_pages_refusals(kw, want):
     assert _pages(**kw) == want
+
+
+def test_linear_plans():
+    # one long sequence is cut, and the room for what its pieces add is asked for; many sequences of the same length are not
+    p = _params(num_seqs=1, total_tokens=30000)
+    cu = np.array([0, 30000], np.int32)
+    need = up.uniprefill_linear_attention_plan(p, cu)[1]
+    assert 0 < need < 1 << 30
+    kw = dict(cu_host=cu, out_stride=8 * 128)
+    assert _linear(p, ws=None, **kw) == up.UP_ERR_WORKSPACE
+    assert _linear(p, ws_bytes=need - 1, **kw) == up.UP_ERR_WORKSPACE
+    assert _linear(p, ws=A + 16, **kw) == up.UP_ERR_ALIGN
+    n = 1000
+    p = _params(num_seqs=n, total_tokens=50 * n, num_kv_heads=8)
+    assert up.uniprefill_linear_attention_plan(p, np.arange(n + 1, dtype=np.int32) * 50)[1] == 0
+    assert up.uniprefill_linear_attention_plan(p, None, check=False)[0] == up.UP_ERR_NULL
