@@ -69,13 +69,13 @@ struct PagesArgs {
 
 #if defined(__HIPCC__)
 hipError_t launch_linear(const LinearArgs& a, bool f32, int D, hipStream_t s);
-hipError_t launch_linear_tokens(const LinearArgs& a, bool f32, int D, hipStream_t s);
+hipError_t launch_linear_step(const LinearArgs& a, bool f32, int D, hipStream_t s);
 hipError_t launch_rotate(const RotateArgs& a, bool f32, hipStream_t s);
 hipError_t launch_pages(const PagesArgs& a, hipStream_t s);
 #else
 // the host-only build of the argument checks has no kernels to launch
 inline hipError_t launch_linear(const LinearArgs&, bool, int, hipStream_t) { return hipSuccess; }
-inline hipError_t launch_linear_tokens(const LinearArgs&, bool, int, hipStream_t) { return hipSuccess; }
+inline hipError_t launch_linear_step(const LinearArgs&, bool, int, hipStream_t) { return hipSuccess; }
 inline hipError_t launch_rotate(const RotateArgs&, bool, hipStream_t) { return hipSuccess; }
 inline hipError_t launch_pages(const PagesArgs&, hipStream_t) { return hipSuccess; }
 #endif

@@ -200,7 +200,7 @@ int uniprefill_linear_attention_step(const up_params* p, const void* q, const vo
   if (st != UP_OK) return st;
   if (pb.T != pb.R) return UP_ERR_SHAPE;
   if (pb.R == 0) return UP_OK;
-  return launch_linear_tokens(a, pb.qk_is_f32, pb.head_dim, (hipStream_t)stream) == hipSuccess ? UP_OK : UP_ERR_HIP;
+  return launch_linear_step(a, pb.qk_is_f32, pb.head_dim, (hipStream_t)stream) == hipSuccess ? UP_OK : UP_ERR_HIP;
 }
 
 int uniprefill_norm_rotate(const up_params* p, const void* q, const void* k, const void* v, int64_t v_row_stride, const void* q_weight,

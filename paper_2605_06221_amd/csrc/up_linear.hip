@@ -1,7 +1,7 @@
 // Linear attention with a decay for each kv head (lam = exp(log_decay), at most 1):
 //     S_t = lam S_{t-1} + k_t^T v_t,        out_t = scale q_t S_t      (S: D x D, float, carried by the sequence)
 //
-// k_linear_tokens, token after token: a work-group holds 32 columns of a head's state in registers, eight lanes by 32 groups of rows.
+// k_linear_step: one token per sequence.  k_linear, k_linear_join: prompts and chunks, 32 tokens at a time on the matrix cores.
 #include "up_attn.h"
 #include "up_layers.h"
 
@@ -25,67 +25,63 @@ __device__ __forceinline__ long long linear_slot(const int32_t* of, int r, long 
   return s >= 0 && s < num ? s : -1;
 }
 
+// One token per sequence.  A work-group holds 32 columns of a head's state in registers, eight lanes by 32 groups of rows: every row's 128 bytes
+// are read and written whole, and even a single sequence of few heads has work-groups for some tens of CUs.  Bound by the states' bytes
+// (64 sequences of 32 heads of 128: 59 us, 4.6 TB/s, 91 % of a copy's rate; one sequence: a launch).
 template <bool F32, int D>
-__global__ __launch_bounds__(256) void k_linear_tokens(LinearArgs a) {
+__global__ __launch_bounds__(256) void k_linear_step(LinearArgs a) {
   constexpr int SLICES = D / 32, PER = D / 32, E = F32 ? 4 : 2;      // rows of the state per lane
   const int slice = blockIdx.x % SLICES, kvh = (blockIdx.x / SLICES) % a.Hkv, r = blockIdx.x / (SLICES * a.Hkv);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int col = slice * 32 + (lane & 7) * 4, row0 = (wave * 8 + (lane >> 3)) * PER;
   __shared__ f32x4 part[2][4][8];
-  const int c0 = a.cu != nullptr ? a.cu[r] : r, N = a.cu != nullptr ? a.cu[r + 1] - c0 : 1;
   const long long from = linear_slot(a.state_in, r, a.num_states), to = linear_slot(a.state_out, r, a.num_states);
-  f32x4 S[PER];
+  const long long state_at = ((long long)kvh * D + row0) * D + col;
+  const char* k = a.k + (long long)r * a.k_stride_b + (long long)kvh * D * E;
+  const char* v = a.v + (long long)r * a.v_stride_b + (long long)kvh * D * E;
+  f32x4 S[PER], v4;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
     S[i] = f32x4{0, 0, 0, 0};
-    if (from >= 0) S[i] = *(const f32x4*)(a.states + from * a.state_stride + ((long long)kvh * D + row0 + i) * D + col);
+    if (from >= 0) S[i] = *(const f32x4*)(a.states + from * a.state_stride + state_at + i * D);
   }
   float one, lacks;
   linear_decay(a.log_decay[kvh], 1, one, lacks);
-  const float hi = one, lo = one * lacks;
-  int turn = 0;
-  for (int t = c0; t < c0 + N; ++t) {
-    const char* k = a.k + (long long)t * a.k_stride_b + (long long)kvh * D * E;
-    const char* v = a.v + (long long)t * a.v_stride_b + (long long)kvh * D * E;
-    f32x4 v4;
+  const float rest = one * lacks;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v4[i] = linear_load(v, col + i, F32);
+  for (int i = 0; i < 4; ++i) v4[i] = linear_load(v, col + i, F32);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const float ki = linear_load(k, row0 + i, F32);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) S[i][e] = fmaf(ki, v4[e], fmaf(S[i][e], one, S[i][e] * rest));
+    if (to >= 0) *(f32x4*)(a.states + to * a.state_stride + state_at + i * D) = S[i];
+  }
+  for (int g = 0; g < a.Gq; ++g) {
+    const int h = kvh * a.Gq + g;
+    const char* q = a.q + (long long)r * a.q_stride_b + (long long)h * D * E;
+    f32x4 o = {0, 0, 0, 0};
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-      const float ki = linear_load(k, row0 + i, F32);
+      const float qi = linear_load(q, row0 + i, F32);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) S[i][e] = fmaf(ki, v4[e], fmaf(S[i][e], hi, S[i][e] * lo));
+      for (int e = 0; e < 4; ++e) o[e] = fmaf(qi, S[i][e], o[e]);
     }
-    for (int g = 0; g < a.Gq; ++g, turn ^= 1) {
-      const int h = kvh * a.Gq + g;
-      const char* q = a.q + (long long)t * a.q_stride_b + (long long)h * D * E;
-      f32x4 o = {0, 0, 0, 0};
 #pragma unroll
-      for (int i = 0; i < PER; ++i) {
-        const float qi = linear_load(q, row0 + i, F32);
+    for (int e = 0; e < 4; ++e)
+      for (int d = 8; d < 64; d <<= 1) o[e] += __shfl_xor(o[e], d);
+    if (lane < 8) part[g & 1][wave][lane] = o;
+    __syncthreads();      // (two buffers: the readers of this one are through before it is written again)
+    if (tid < 8) {
+      const f32x4 p0 = part[g & 1][0][tid], p1 = part[g & 1][1][tid], p2 = part[g & 1][2][tid], p3 = part[g & 1][3][tid];
+      char* dst = a.out + (long long)r * a.out_stride_b + (long long)h * D * E;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = fmaf(qi, S[i][e], o[e]);
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        for (int d = 8; d < 64; d <<= 1) o[e] += __shfl_xor(o[e], d);
-      if (lane < 8) part[turn][wave][lane] = o;
-      __syncthreads();      // (two buffers: the readers of this one are through before it is written again)
-      if (tid < 8) {
-        const f32x4 p0 = part[turn][0][tid], p1 = part[turn][1][tid], p2 = part[turn][2][tid], p3 = part[turn][3][tid];
-        char* dst = a.out + (long long)t * a.out_stride_b + (long long)h * D * E;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float y = ((p0[e] + p1[e]) + (p2[e] + p3[e])) * a.scale;
-          if (F32) ((float*)dst)[col + e] = y;
-          else ((__bf16*)dst)[col + e] = (__bf16)y;
-        }
+      for (int e = 0; e < 4; ++e) {
+        const float y = ((p0[e] + p1[e]) + (p2[e] + p3[e])) * a.scale;
+        if (F32) ((float*)dst)[col + e] = y;
+        else ((__bf16*)dst)[col + e] = (__bf16)y;
       }
     }
-  }
-  if (to >= 0) {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) *(f32x4*)(a.states + to * a.state_stride + ((long long)kvh * D + row0 + i) * D + col) = S[i];
   }
 }
 
@@ -103,7 +99,14 @@ __global__ __launch_bounds__(256) void k_linear_tokens(LinearArgs a) {
 // in two parts of bf16 (16 bits), V' the one for the state in three (24 bits: what the state adds up over a long sequence stays float).
 //
 // Long sequences are cut into pieces of `piece` tokens: one launch leaves what every piece adds to the state, a second
-// adds these up in order, and the third walks over the pieces from the states that they begin with.
+// adds these up in order, and the third walks over the pieces from the states that they begin with.  Keys and values are then read twice.
+//
+// What bounds it: at one query head per kv head the bytes (a prompt of 32768, 32 heads of 128: 115 us for the first launch, 537 MB, and 230 for the
+// third, 1.07 GB, 4.7 TB/s both, 20 for the second; 410 in all), with the SIMDs full as well (matrix cores busy in 40 % of
+// the cycles, vector pipe in 63 %: most of that is taking the state apart).  With several query heads per kv head the vector work: 32/8 heads 259 us.
+// What it took (the same prompt): token after token 40.8 ms; chunks through registers into LDS, states scaled every chunk 490 us; two buffers and
+// one barrier a chunk 469; straight into LDS, scaled when needed, three work-groups a CU instead of two 408.  The state's parts kept
+// over the query heads, 16-byte stores and no wait for them: 32/8 heads 292 -> 259 us.
 constexpr int kLinearChunk = 32;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -546,15 +549,15 @@ hipError_t launch_linear(const LinearArgs& a, bool f32, int D, hipStream_t s) {
 }
 
 template <bool F32, int D>
-static hipError_t launch_linear_tokens_form(const LinearArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((k_linear_tokens<F32, D>), dim3((unsigned)a.R * a.Hkv * (D / 32)), dim3(256), 0, s, a);
+static hipError_t launch_linear_step_form(const LinearArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((k_linear_step<F32, D>), dim3((unsigned)a.R * a.Hkv * (D / 32)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
-hipError_t launch_linear_tokens(const LinearArgs& a, bool f32, int D, hipStream_t s) {
-  if (f32) return D == 64 ? launch_linear_tokens_form<true, 64>(a, s) : launch_linear_tokens_form<true, 128>(a, s);
-  return D == 64 ? launch_linear_tokens_form<false, 64>(a, s) : D == 128 ? launch_linear_tokens_form<false, 128>(a, s)
-                                                                         : launch_linear_tokens_form<false, 256>(a, s);
+hipError_t launch_linear_step(const LinearArgs& a, bool f32, int D, hipStream_t s) {
+  if (f32) return D == 64 ? launch_linear_step_form<true, 64>(a, s) : launch_linear_step_form<true, 128>(a, s);
+  return D == 64 ? launch_linear_step_form<false, 64>(a, s) : D == 128 ? launch_linear_step_form<false, 128>(a, s)
+                                                                         : launch_linear_step_form<false, 256>(a, s);
 }
 
 }  // namespace up
