@@ -509,12 +509,21 @@ __global__ __launch_bounds__(256) void k_linear_join(LinearArgs a) {
   float* add = linear_add(a, w, D) + at;
   float one, lacks;
   linear_decay(a.log_decay[kvh], a.piece, one, lacks);
-  int left = w.length;
-  for (; left > a.piece; left -= a.piece, add += step) {
-    const f32x4 x = *(const f32x4*)add;
-    *(f32x4*)add = S;
+  // (eight pieces' sums are under way together; the last piece's is added below, if anybody asks)
+  const int before_last = (w.length - 1) / a.piece, left = w.length - before_last * a.piece;
+  for (int i = 0; i < before_last; i += 8) {
+    f32x4 x[8];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) S[e] = fmaf(S[e], one, fmaf(S[e], one * lacks, x[e]));
+    for (int u = 0; u < 8; ++u)
+      if (i + u < before_last) x[u] = *(const f32x4*)(add + u * step);
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (i + u >= before_last) break;
+      *(f32x4*)add = S;
+      add += step;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) S[e] = fmaf(S[e], one, fmaf(S[e], one * lacks, x[u][e]));
+    }
   }
   if (to >= 0) {
     const f32x4 x = *(const f32x4*)add;
