@@ -102,11 +102,12 @@ __global__ __launch_bounds__(256) void k_linear_step(LinearArgs a) {
 // adds these up in order, and the third walks over the pieces from the states that they begin with.  Keys and values are then read twice.
 //
 // What bounds it: at one query head per kv head the bytes (a prompt of 32768, 32 heads of 128: 115 us for the first launch, 537 MB, and 230 for the
-// third, 1.07 GB, 4.7 TB/s both, 20 for the second; 410 in all), with the SIMDs full as well (matrix cores busy in 40 % of
-// the cycles, vector pipe in 63 %: most of that is taking the state apart).  With several query heads per kv head the vector work: 32/8 heads 259 us.
+// third, 1.07 GB, 4.7 TB/s both, 20 for the second; 410 to 430 in all), with the SIMDs full as well (matrix cores busy in 40 % of
+// the cycles, vector pipe in 63 %: most of that is taking the state apart).  With several query heads per kv head a step's own latency, about 2 us
+// from tiles to outputs, with few waves to fill it (40/8 heads of 64: matrix cores busy in 16 % of the cycles, vector pipe in 23 %): 32/8 heads 245 us.
 // What it took (the same prompt): token after token 40.8 ms; chunks through registers into LDS, states scaled every chunk 490 us; two buffers and
 // one barrier a chunk 469; straight into LDS, scaled when needed, three work-groups a CU instead of two 408.  The state's parts kept
-// over the query heads, 16-byte stores and no wait for them: 32/8 heads 292 -> 259 us.
+// over the query heads, 16-byte stores and no wait for them: 32/8 heads 292 -> 259 us; eight pieces under way in the join: 8000 tokens of 8/8 heads of 64 40 -> 30.
 constexpr int kLinearChunk = 32;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));

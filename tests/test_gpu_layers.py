@@ -340,6 +340,17 @@ def test_linear_attention_of_long_sequences(D, dtype):
     b.check()
 
 
+@pytest.mark.parametrize("D,dtype", [(64, BF), (256, BF), (128, F32)])
+def test_linear_attention_at_the_borders_of_pieces(D, dtype):
+    # pieces of 64 tokens: one, two, eight, nine and seventeen whole ones, and a token more or less
+    lengths = [64, 65, 128, 512, 513, 576, 577, 1088, 1087]
+    _say("linear attention, whole pieces", D, dtype)
+    starts, stores = _slots(len(lengths))
+    b = Linear(29, lengths, 2, 1, D, dtype, log_decay=[-0.01], starts=starts, stores=stores)
+    b.run()
+    b.check()
+
+
 def test_linear_attention_without_states_with_a_scale_and_in_two_calls():
     _say("linear attention: no pool, scale; one call against two")
     b = Linear(5, [150, 40], 4, 2, 128, scale=1.0)
