@@ -742,7 +742,10 @@ int uniprefill_norm_rotate(const up_params* p, const void* q, const void* k, con
  *                    cu_seqlens), cu_seqlens_k_dev those of the keys (new_len_dev added up; sums beyond
  *                    2^31 - 1 are written as that)
  *   pos, slots       [capacity] int32 position and int64 slot of every token served, in order; the rest
- *                    is filled with 0 and -1, the slot that the cache's entry points leave out
+ *                    is filled with 0 and -1, the slot that the cache's entry points leave out.  Positions
+ *                    are places in the cache, which is right where the cache holds all of a
+ *                    sequence's tokens; behind a drop, or after an eviction, see
+ *                    uniprefill_append_pages_dropped
  *   num_served_dev   [1] sequences served
  * The arrays overlap in no other way.  Lengths beyond what a row of the table holds are not served; entries of the table up to a sequence's
  * length must name its pages.  capacity and num_seqs up to 2^31 - 65537 (UP_ERR_UNSUPPORTED),
@@ -752,6 +755,22 @@ int uniprefill_append_pages(const int32_t* kv_len_dev, const int32_t* num_new_de
                             const int32_t* free_pages, const int32_t* num_free_dev, int32_t* free_left_dev,
                             int32_t* new_len_dev, int32_t* cu_seqlens_dev, int32_t* cu_seqlens_k_dev, int32_t* pos,
                             int64_t* slots, int64_t capacity, int32_t* num_served_dev, void* stream);
+
+/* The same for a cache that does not hold all tokens of its sequences (the layers
+ * behind a drop, a cache after uniprefill_cache_evict): num_dropped_dev[r] (int32
+ * [num_seqs] on the device; negative values count as 0; NULL: none) tokens of sequence r stand
+ * before the new ones and are not among its kv_len_dev[r] cached ones.  A new token's
+ * position, the one by which uniprefill_norm_rotate has to turn it, is then its place in the
+ * cache plus that number (beyond 2^31 - 1: that); all else is as above.  The number stays
+ * the same from one decode step to the next.  (The retained tokens of a prompt or chunk
+ * lie apart in their request: their positions are those that the drop has compacted, not
+ * this call's.) */
+int uniprefill_append_pages_dropped(const int32_t* kv_len_dev, const int32_t* num_new_dev,
+                                    const int32_t* num_dropped_dev, int32_t num_seqs, int32_t kv_block_size,
+                                    int32_t* block_table, int64_t block_table_stride, const int32_t* free_pages,
+                                    const int32_t* num_free_dev, int32_t* free_left_dev, int32_t* new_len_dev,
+                                    int32_t* cu_seqlens_dev, int32_t* cu_seqlens_k_dev, int32_t* pos, int64_t* slots,
+                                    int64_t capacity, int32_t* num_served_dev, void* stream);
 
 /* Static, never NULL. */
 const char* uniprefill_status_string(int status);

@@ -94,8 +94,8 @@ def norm_rotate(x, weight, eps, pos, inv_freq, rot_dim, pairs):
     return out, size
 
 
-def append_pages(kv_len, num_new, page, table, free_pages, num_free, capacity):
-    """dict of what uniprefill_append_pages writes, a request at a time."""
+def append_pages(kv_len, num_new, page, table, free_pages, num_free, capacity, dropped=None):
+    """dict of what uniprefill_append_pages (dropped: _append_pages_dropped) writes, a request at a time."""
     table, free = np.array(table, np.int64), [int(x) for x in free_pages[:max(0, num_free)]]
     new_len, cu, cu_k, pos, slots, served, going = [], [0], [0], [], [], 0, True
     for r in range(len(kv_len)):
@@ -110,7 +110,7 @@ def append_pages(kv_len, num_new, page, table, free_pages, num_free, capacity):
             for j in range(need):
                 table[r, have + j] = free.pop()
         for p in range(n, n + add):
-            pos.append(p)
+            pos.append(min(p + (0 if dropped is None else max(0, int(dropped[r]))), 2 ** 31 - 1))
             slots.append(int(table[r, p // page]) * page + p % page)
         new_len.append(n + add)
         cu.append(cu[-1] + add)

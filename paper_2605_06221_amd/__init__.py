@@ -12,7 +12,7 @@ from .binding import (  # noqa: F401
     uniprefill_cache_load_q4, uniprefill_attention_q4_plan, uniprefill_attention_q4, uniprefill_cache_evict,
     uniprefill_attention_window_plan, uniprefill_attention_window, uniprefill_attention_window_step_plan,
     uniprefill_attention_window_step, uniprefill_linear_attention_plan, uniprefill_linear_attention, uniprefill_linear_attention_step,
-    uniprefill_norm_rotate, uniprefill_append_pages,
+    uniprefill_norm_rotate, uniprefill_append_pages, uniprefill_append_pages_dropped,
     UP_PHASE_PLAN, UP_PHASE_ROW_STATS, UP_PHASE_MERGE_STATS, UP_PHASE_SWEEP_SELECT, UP_PHASE_GATHER,
     UP_PHASE_ALL, UP_PHASE_GATHER_IN_SELECT,
 )

@@ -33,6 +33,7 @@ EXPORTS = ["uniprefill_plan", "uniprefill_score", "uniprefill_select", "uniprefi
            "uniprefill_cache_evict", "uniprefill_attention_window_plan", "uniprefill_attention_window",
            "uniprefill_attention_window_step_plan", "uniprefill_attention_window_step", "uniprefill_linear_attention_plan",
            "uniprefill_linear_attention", "uniprefill_linear_attention_step", "uniprefill_norm_rotate", "uniprefill_append_pages",
+           "uniprefill_append_pages_dropped",
            "uniprefill_status_string"]
 
 UP_PHASE_PLAN, UP_PHASE_ROW_STATS, UP_PHASE_MERGE_STATS, UP_PHASE_SWEEP_SELECT, UP_PHASE_GATHER = 1, 2, 4, 8, 16
@@ -123,7 +124,9 @@ def _load():
     lib.uniprefill_linear_attention_step.argtypes = [P, vp, vp, vp, i64] + states + [vp, i64, vp]
     lib.uniprefill_norm_rotate.argtypes = [P, vp, vp, vp, i64, vp, vp, f32, i32p, f32p, i32, i32, i32p, vp, i64, vp, i64, vp, i64, vp, i64,
                                            vp]
-    lib.uniprefill_append_pages.argtypes = [i32p, i32p, i32, i32, i32p, i64, i32p, i32p, i32p, i32p, i32p, i32p, i32p, vp, i64, i32p, vp]
+    pages = [i32, i32, i32p, i64, i32p, i32p, i32p, i32p, i32p, i32p, i32p, vp, i64, i32p, vp]
+    lib.uniprefill_append_pages.argtypes = [i32p, i32p] + pages
+    lib.uniprefill_append_pages_dropped.argtypes = [i32p, i32p, i32p] + pages
     for name in EXPORTS[:-1]:
         getattr(lib, name).restype = ctypes.c_int
     lib.uniprefill_q4_row_bytes.restype = i64
@@ -621,3 +624,14 @@ def uniprefill_append_pages(kv_len_dev, num_new_dev, num_seqs, kv_block_size, bl
                                       _addr(new_len_dev), _addr(cu_seqlens_dev), _addr(cu_seqlens_k_dev), _addr(pos), _addr(slots),
                                       int(capacity), _addr(num_served_dev), _stream(stream))
     return _check(st, "uniprefill_append_pages", check)
+
+
+def uniprefill_append_pages_dropped(kv_len_dev, num_new_dev, num_dropped_dev, num_seqs, kv_block_size, block_table, block_table_stride,
+                                    free_pages, num_free_dev, free_left_dev, new_len_dev, cu_seqlens_dev, cu_seqlens_k_dev, pos, slots,
+                                    capacity, num_served_dev, stream=None, check=True):
+    st = _lib.uniprefill_append_pages_dropped(_addr(kv_len_dev), _addr(num_new_dev), _addr(num_dropped_dev), int(num_seqs),
+                                              int(kv_block_size), _addr(block_table), int(block_table_stride), _addr(free_pages),
+                                              _addr(num_free_dev), _addr(free_left_dev), _addr(new_len_dev), _addr(cu_seqlens_dev),
+                                              _addr(cu_seqlens_k_dev), _addr(pos), _addr(slots), int(capacity), _addr(num_served_dev),
+                                              _stream(stream))
+    return _check(st, "uniprefill_append_pages_dropped", check)

@@ -50,6 +50,7 @@ struct RotateArgs {
 struct PagesArgs {
   const int32_t* kv_len;
   const int32_t* num_new;
+  const int32_t* dropped;          // [R] tokens of a sequence that the cache does not hold; nullptr: none
   const int32_t* free_pages;
   const int32_t* num_free;
   int32_t* block_table;

@@ -77,6 +77,33 @@ int linear_geometry(const Problem& pb, const int32_t* cu, LinearGeometry* g) {
   return UP_OK;
 }
 
+// ---- pages for new tokens
+int append_pages_impl(const int32_t* kv_len_dev, const int32_t* num_new_dev, const int32_t* num_dropped_dev, int32_t num_seqs, int32_t kv_block_size,
+                      int32_t* block_table, int64_t block_table_stride, const int32_t* free_pages, const int32_t* num_free_dev,
+                      int32_t* free_left_dev, int32_t* new_len_dev, int32_t* cu_seqlens_dev, int32_t* cu_seqlens_k_dev, int32_t* pos,
+                      int64_t* slots, int64_t capacity, int32_t* num_served_dev, void* stream) {
+  if (num_seqs < 0 || capacity < 0) return UP_ERR_SHAPE;
+  if (kv_block_size < 1 || block_table_stride < 0) return UP_ERR_RANGE;
+  if (!num_free_dev || !free_left_dev || !cu_seqlens_dev || !cu_seqlens_k_dev || !num_served_dev) return UP_ERR_NULL;
+  if (num_seqs > 0 && (!kv_len_dev || !num_new_dev || !new_len_dev || !free_pages || (block_table_stride > 0 && !block_table))) return UP_ERR_NULL;
+  if (capacity > 0 && (!pos || !slots)) return UP_ERR_NULL;
+  if (!aligned_to(kv_len_dev, 4) || !aligned_to(num_new_dev, 4) || !aligned_to(num_dropped_dev, 4) || !aligned_to(block_table, 4) || !aligned_to(free_pages, 4) ||
+      !aligned_to(num_free_dev, 4) || !aligned_to(free_left_dev, 4) || !aligned_to(new_len_dev, 4) || !aligned_to(cu_seqlens_dev, 4) ||
+      !aligned_to(cu_seqlens_k_dev, 4) || !aligned_to(pos, 4) || !aligned_to(slots, 8) || !aligned_to(num_served_dev, 4))
+    return UP_ERR_ALIGN;
+  if (capacity > INT32_MAX - 65536 || num_seqs > INT32_MAX - 65536) return UP_ERR_UNSUPPORTED;
+  // the lengths may be updated in place, and so may the count of free pages; they overlap in no other way
+  const intptr_t apart = (intptr_t)new_len_dev - (intptr_t)kv_len_dev, ends = (intptr_t)num_seqs * (intptr_t)sizeof(int32_t);
+  if (apart != 0 && apart > -ends && apart < ends) return UP_ERR_UNSUPPORTED;
+  PagesArgs a{};
+  a.kv_len = kv_len_dev; a.num_new = num_new_dev; a.dropped = num_dropped_dev; a.free_pages = free_pages; a.num_free = num_free_dev;
+  a.block_table = block_table; a.table_stride = block_table_stride; a.free_left = free_left_dev; a.new_len = new_len_dev;
+  a.cu = cu_seqlens_dev; a.cu_k = cu_seqlens_k_dev; a.pos = pos; a.slots = slots; a.served = num_served_dev;
+  a.capacity = capacity; a.R = num_seqs; a.kv_block = kv_block_size;
+  a.kv_magic = 0xFFFFFFFFu / (unsigned)kv_block_size;
+  return launch_pages(a, (hipStream_t)stream) == hipSuccess ? UP_OK : UP_ERR_HIP;
+}
+
 }  // namespace
 
 extern "C" {
@@ -257,26 +284,16 @@ int uniprefill_append_pages(const int32_t* kv_len_dev, const int32_t* num_new_de
                             const int32_t* num_free_dev, int32_t* free_left_dev, int32_t* new_len_dev, int32_t* cu_seqlens_dev,
                             int32_t* cu_seqlens_k_dev, int32_t* pos, int64_t* slots, int64_t capacity, int32_t* num_served_dev,
                             void* stream) {
-  if (num_seqs < 0 || capacity < 0) return UP_ERR_SHAPE;
-  if (kv_block_size < 1 || block_table_stride < 0) return UP_ERR_RANGE;
-  if (!num_free_dev || !free_left_dev || !cu_seqlens_dev || !cu_seqlens_k_dev || !num_served_dev) return UP_ERR_NULL;
-  if (num_seqs > 0 && (!kv_len_dev || !num_new_dev || !new_len_dev || !free_pages || (block_table_stride > 0 && !block_table))) return UP_ERR_NULL;
-  if (capacity > 0 && (!pos || !slots)) return UP_ERR_NULL;
-  if (!aligned_to(kv_len_dev, 4) || !aligned_to(num_new_dev, 4) || !aligned_to(block_table, 4) || !aligned_to(free_pages, 4) ||
-      !aligned_to(num_free_dev, 4) || !aligned_to(free_left_dev, 4) || !aligned_to(new_len_dev, 4) || !aligned_to(cu_seqlens_dev, 4) ||
-      !aligned_to(cu_seqlens_k_dev, 4) || !aligned_to(pos, 4) || !aligned_to(slots, 8) || !aligned_to(num_served_dev, 4))
-    return UP_ERR_ALIGN;
-  if (capacity > INT32_MAX - 65536 || num_seqs > INT32_MAX - 65536) return UP_ERR_UNSUPPORTED;
-  // the lengths may be updated in place, and so may the count of free pages; they overlap in no other way
-  const intptr_t apart = (intptr_t)new_len_dev - (intptr_t)kv_len_dev, ends = (intptr_t)num_seqs * (intptr_t)sizeof(int32_t);
-  if (apart != 0 && apart > -ends && apart < ends) return UP_ERR_UNSUPPORTED;
-  PagesArgs a{};
-  a.kv_len = kv_len_dev; a.num_new = num_new_dev; a.free_pages = free_pages; a.num_free = num_free_dev;
-  a.block_table = block_table; a.table_stride = block_table_stride; a.free_left = free_left_dev; a.new_len = new_len_dev;
-  a.cu = cu_seqlens_dev; a.cu_k = cu_seqlens_k_dev; a.pos = pos; a.slots = slots; a.served = num_served_dev;
-  a.capacity = capacity; a.R = num_seqs; a.kv_block = kv_block_size;
-  a.kv_magic = 0xFFFFFFFFu / (unsigned)kv_block_size;
-  return launch_pages(a, (hipStream_t)stream) == hipSuccess ? UP_OK : UP_ERR_HIP;
+  return append_pages_impl(kv_len_dev, num_new_dev, nullptr, num_seqs, kv_block_size, block_table, block_table_stride, free_pages, num_free_dev,
+                           free_left_dev, new_len_dev, cu_seqlens_dev, cu_seqlens_k_dev, pos, slots, capacity, num_served_dev, stream);
+}
+
+int uniprefill_append_pages_dropped(const int32_t* kv_len_dev, const int32_t* num_new_dev, const int32_t* num_dropped_dev, int32_t num_seqs, int32_t kv_block_size,
+                                    int32_t* block_table, int64_t block_table_stride, const int32_t* free_pages, const int32_t* num_free_dev,
+                                    int32_t* free_left_dev, int32_t* new_len_dev, int32_t* cu_seqlens_dev, int32_t* cu_seqlens_k_dev, int32_t* pos,
+                                    int64_t* slots, int64_t capacity, int32_t* num_served_dev, void* stream) {
+  return append_pages_impl(kv_len_dev, num_new_dev, num_dropped_dev, num_seqs, kv_block_size, block_table, block_table_stride, free_pages, num_free_dev,
+                           free_left_dev, new_len_dev, cu_seqlens_dev, cu_seqlens_k_dev, pos, slots, capacity, num_served_dev, stream);
 }
 
 }  // extern "C"

@@ -38,6 +38,13 @@ __device__ __forceinline__ int pages_of(const PagesArgs& a, int n) {
   return (int)whole + (rest != 0);
 }
 
+// The position of the token at place p of sequence r's cache: the tokens that the cache does not hold stand before it.
+__device__ __forceinline__ int pages_position(const PagesArgs& a, int r, int p) {
+  if (a.dropped == nullptr) return p;
+  const long long at = (long long)p + imax(0, a.dropped[r]);
+  return at > INT32_MAX ? INT32_MAX : (int)at;
+}
+
 // the first of n ends that lies behind x
 __device__ __forceinline__ int first_past(const int* end, int n, int x) {
   int lo = 0, hi = n - 1;
@@ -158,6 +165,7 @@ __global__ __launch_bounds__(kPagesThreads) void k_pages(PagesArgs a) {
           const int id = j < had ? a.block_table[(long long)s * a.table_stride + j]
                                  : a.free_pages[free_at_start - 1 - (s > 0 ? page_end[s - 1] : 0) - (int)(j - had)];
           slot = (int64_t)id * a.kv_block + at;
+          p = pages_position(a, s, p);
         }
         a.pos[t] = p;
         a.slots[t] = slot;
@@ -195,6 +203,7 @@ __global__ __launch_bounds__(256) void k_pages_slots(PagesArgs a) {
     unsigned j, at;
     divmod_by((unsigned)p, (unsigned)a.kv_block, a.kv_magic, j, at);
     slot = (int64_t)a.block_table[(long long)r * a.table_stride + j] * a.kv_block + at;
+    p = pages_position(a, r, p);
   }
   a.pos[t] = p;
   a.slots[t] = slot;
