@@ -716,11 +716,13 @@ int uniprefill_linear_attention_step(const up_params* p, const void* q, const vo
  *   pos                int32 [T]; inv_freq float [rot_dim / 2], both on the device
  *   rot_dim            0 (nothing turns; pos, inv_freq may be NULL) to head_dim (UP_ERR_RANGE), a
  *                      multiple of 16 (UP_ERR_UNSUPPORTED)
- *   q_out              row t in place t; may be q itself (same stride).  Otherwise outputs overlap no input
+ *   q_out              row t in place t; may be q itself with the same stride.  Otherwise outputs overlap no
+ *                      input: an output at its input's address with another stride, or by slots, is
+ *                      UP_ERR_UNSUPPORTED
  *   k_out, v_out       row t in place slots[t] (int64, as uniprefill_slot_mapping and
  *                      uniprefill_append_pages write them; rows whose slot lies outside
  *                      [0, num_slots) are left out, no slot may be named twice), or with slots NULL in place t
- *                      (k_out may then be k itself)
+ *                      (k_out may then be k itself with the same stride, and v_out v)
  * Squares of a row must stay within float. */
 int uniprefill_norm_rotate(const up_params* p, const void* q, const void* k, const void* v, int64_t v_row_stride,
                            const void* q_weight, const void* k_weight, float eps, const int32_t* pos,

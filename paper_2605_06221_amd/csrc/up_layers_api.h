@@ -257,6 +257,14 @@ int uniprefill_norm_rotate(const up_params* p, const void* q, const void* k, con
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(q_out) || !aligned16(k_out) || !aligned16(v_out)) return UP_ERR_ALIGN;
   if (!aligned16(q_weight) || !aligned16(k_weight) || !aligned_to(pos, 4) || !aligned_to(inv_freq, 4)) return UP_ERR_ALIGN;
   if (!aligned_to(slots, 8) || !aligned_to(count_dev, 4)) return UP_ERR_ALIGN;
+  // Rows are turned where they are only if they stay in their places: with another stride, or by slots, a wave would write a row that
+  // another one has still to read.
+  auto moves = [&](const void* in, int64_t in_stride, const void* out, int64_t out_stride, bool by_slots) {
+    return in != nullptr && in == out && (by_slots || in_stride != out_stride);
+  };
+  if (pb.T > 1 && (moves(q, pb.q_stride, q_out, q_out_row_stride, false) || moves(k, pb.k_stride, k_out, k_out_row_stride, slots != nullptr) ||
+                   moves(v, v_row_stride, v_out, v_out_row_stride, slots != nullptr)))
+    return UP_ERR_UNSUPPORTED;
   RotateArgs a{};
   a.in[0] = (const char*)q; a.in[1] = (const char*)k; a.in[2] = (const char*)v;
   a.out[0] = (char*)q_out; a.out[1] = (char*)k_out; a.out[2] = (char*)v_out;
