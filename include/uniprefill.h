@@ -678,7 +678,9 @@ int uniprefill_attention_window_step(const up_params* p, const void* q, const vo
  *   A sequence may start from the slot it stores to.  A slot that one sequence stores to
  *   must be named by no other sequence of the call.
  * States are float throughout: bf16 products are exact, the decayed keys and values keep
- * 24 bits.  In the outputs the decayed logits and the state are taken in 16 bits.
+ * 24 bits (state elements and values below 2^-80 fewer).  In the outputs the decayed logits and
+ * the state are taken in 16 bits.  Rows and states must be finite, and so must the sums of their
+ * products be in float; log_decay may be -infinity, but no NaN.
  *   out          as for uniprefill_attention; overlaps none of q, k, v
  *   workspace    from uniprefill_linear_attention_plan with the same lengths
  *                (256-byte aligned; 0 bytes, and NULL, where no sequence is cut)

@@ -109,6 +109,7 @@ __global__ __launch_bounds__(256) void k_linear_step(LinearArgs a) {
 // one barrier a chunk 469; straight into LDS, scaled when needed, three work-groups a CU instead of two 408.  The state's parts kept
 // over the query heads, 16-byte stores and no wait for them: 32/8 heads 292 -> 259 us; eight pieces under way in the join: 8000 tokens of 8/8 heads of 64 40 -> 30.
 constexpr int kLinearChunk = 32;
+constexpr float kLinearUnit = 0x1p24f;      // what the state is divided by when it was last scaled (below)
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -230,8 +231,9 @@ __global__ __launch_bounds__(64 * (D / 32), (HOLD && D == 128 ? 2 : LinearTile<F
   auto weigh = [&](int m) {      // (tokens past the chunk's m weigh nothing)
     if (tid < kLinearChunk) value_weight[tid] = tid < m ? __builtin_amdgcn_exp2f(ldf * (float)(m - 1 - tid)) : 0.0f;
   };
-  // The state stands in registers as S / f, f = lam^(tokens since they were last scaled): it is scaled when f has passed 2^-24, not with
-  // every chunk.
+  // The state stands in registers as S / (2^24 f), f = lam^(tokens since they were last scaled): it is scaled when f has passed 2^-24, not with
+  // every chunk.  (The power of two changes no rounding: with it what stands there is never larger than the state itself, and a state
+  // near the end of float's range does not leave it.  At the other end, below 2^-80, its low bits are lost.)
   int since = 0;
   float f = 1.0f;
 
@@ -341,7 +343,7 @@ __global__ __launch_bounds__(64 * (D / 32), (HOLD && D == 128 ? 2 : LinearTile<F
       }
       __builtin_amdgcn_sched_barrier(0);      // (the operands of one step at a time: all of them at once push accumulators into scratch)
     }
-    const float wof = wo * f;
+    const float wof = wo * (f * kLinearUnit);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       P[e] *= wp[e];
@@ -385,7 +387,7 @@ __global__ __launch_bounds__(64 * (D / 32), (HOLD && D == 128 ? 2 : LinearTile<F
   // the state goes past the chunk: S += K^T V'.  In three parts where it is stored, in two where it only makes outputs.
   auto advance = [&](int m, const u32x4* sk, const u32x4* sv) __attribute__((always_inline)) {
     since += m;
-    f = ldf * (float)since > -120.0f ? linear_power(ld, since) : 0.0f;      // (what stands in S is up to 2^24 times the state)
+    f = ldf * (float)since > -120.0f ? linear_power(ld, since) : 0.0f;      // (past 2^-120 nothing of it is left beside new tokens)
     f = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, f)));      // (the same for the whole wave: a branch)
     if (f < 0x1p-24f) {
 #pragma unroll
@@ -395,7 +397,7 @@ __global__ __launch_bounds__(64 * (D / 32), (HOLD && D == 128 ? 2 : LinearTile<F
       since = 0;
       f = 1.0f;
     }
-    const float inv = 1.0f / f;
+    const float inv = (1.0f / kLinearUnit) / f;
     if constexpr (F32) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
@@ -475,6 +477,12 @@ __global__ __launch_bounds__(64 * (D / 32), (HOLD && D == 128 ? 2 : LinearTile<F
     };
     stage(0, 0, tiles0);
     __builtin_amdgcn_s_waitcnt(0x0f70);
+    if (OUT) {      // (here, where the loads are waited for anyway)
+#pragma unroll
+      for (int kt = 0; kt < T::KT; ++kt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) S[kt][e] *= 1.0f / kLinearUnit;
+    }
     __syncthreads();
     bool more;      // (one way out: a second one costs a second state in registers)
     do {
@@ -484,10 +492,11 @@ __global__ __launch_bounds__(64 * (D / 32), (HOLD && D == 128 ? 2 : LinearTile<F
   }
   float* dst = !OUT ? linear_add(a, w, D) : !cut && to >= 0 ? a.states + to * a.state_stride : nullptr;
   if (dst != nullptr) {
+    const float unit = w.tokens > 0 ? f * kLinearUnit : 1.0f;
 #pragma unroll
     for (int kt = 0; kt < T::KT; ++kt) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) dst[state_at + (32 * kt + 8 * (e >> 2) + (e & 3)) * D] = S[kt][e] * f;
+      for (int e = 0; e < 16; ++e) dst[state_at + (32 * kt + 8 * (e >> 2) + (e & 3)) * D] = S[kt][e] * unit;
       __builtin_amdgcn_sched_barrier(0);
     }
   }
