@@ -136,7 +136,8 @@ __global__ __launch_bounds__(256) void k_rotate(RotateArgs a) {
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      if (type[i] < 2) {
+      // (elements that are neither normalised nor turned stay as they are: a turn by nothing would lose the sign of a zero)
+      if (type[i] < 2 && (turns || a.eps > 0.0f)) {
         float x[VE], y[VE];
         rotate_unpack<F32>(wa[i], x);
         rotate_unpack<F32>(wb[i], y);
