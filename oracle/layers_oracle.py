@@ -77,6 +77,42 @@ def linear_attention(q, k, v, cu_seqlens, log_decay, states=None, state_in=None,
     return out, pool, bound, pool_bound
 
 
+
+def linear_attention_in_chunks(q, k, v, cu_seqlens, log_decay, states=None, state_in=None, state_out=None, *, scale=None, chunk=64):
+    """linear_attention for long sequences: the same sums, `chunk` tokens at a time as matrix products."""
+    cu = np.asarray(cu_seqlens, np.int64)
+    T, Hq, D = q.shape
+    Hkv = k.shape[1]
+    scale = 1.0 / math.sqrt(D) if scale is None else float(np.float32(scale))
+    out, bound = np.zeros((T, Hq, D)), np.zeros((T, Hq, D))
+    pool = None if states is None else np.array(states, np.float64)
+    pool_bound = None if pool is None else np.zeros_like(pool)
+    num = 0 if pool is None else pool.shape[0]
+    for r in range(len(cu) - 1):
+        source, to = (-1 if x is None else int(x[r]) for x in (state_in, state_out))
+        for h in range(Hkv):
+            ld = min(float(log_decay[h]), 0.0)
+            S = states[source, h].astype(np.float64) if 0 <= source < num else np.zeros((D, D))
+            A = np.abs(S)
+            for lo in range(int(cu[r]), int(cu[r + 1]), chunk):
+                hi = min(lo + chunk, int(cu[r + 1]))
+                i = np.arange(hi - lo)
+                age = (i[:, None] - i)
+                w = np.where(age >= 0, np.exp(ld * np.maximum(age, 0)), 0.0)
+                before, after = np.exp(ld * (i + 1.0))[:, None], np.exp(ld * (hi - lo - 1.0 - i))[:, None]
+                K, V = k[lo:hi, h].astype(np.float64), v[lo:hi, h].astype(np.float64)
+                for g in range(h * Hq // Hkv, (h + 1) * Hq // Hkv):
+                    Q = q[lo:hi, g].astype(np.float64)
+                    out[lo:hi, g] = scale * ((Q @ K.T * w) @ V + before * (Q @ S))
+                    bound[lo:hi, g] = scale * ((np.abs(Q) @ np.abs(K).T * w) @ np.abs(V) + before * (np.abs(Q) @ A))
+                last = math.exp(ld * (hi - lo))
+                S = last * S + (K * after).T @ V
+                A = last * A + (np.abs(K) * after).T @ np.abs(V)
+            if 0 <= to < num:
+                pool[to, h], pool_bound[to, h] = S, A
+    return out, pool, bound, pool_bound
+
+
 def norm_rotate(x, weight, eps, pos, inv_freq, rot_dim, pairs):
     """Rows x [T, H, D] normalised (eps > 0) and turned; and |a| + |b| of every element's pair before the turn, for tests."""
     y = np.asarray(x, np.float64)
