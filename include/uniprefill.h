@@ -725,7 +725,7 @@ int uniprefill_linear_attention_step(const up_params* p, const void* q, const vo
  *                      uniprefill_append_pages write them; rows whose slot lies outside
  *                      [0, num_slots) are left out, no slot may be named twice), or with slots NULL in place t
  *                      (k_out may then be k itself with the same stride, and v_out v)
- * Squares of a row must stay within float. */
+ * Squares of a row must stay within float.  More than 67108607 tokens: UP_ERR_UNSUPPORTED. */
 int uniprefill_norm_rotate(const up_params* p, const void* q, const void* k, const void* v, int64_t v_row_stride,
                            const void* q_weight, const void* k_weight, float eps, const int32_t* pos,
                            const float* inv_freq, int32_t rot_dim, int32_t pairs, const int32_t* count_dev,
@@ -751,7 +751,8 @@ int uniprefill_norm_rotate(const up_params* p, const void* q, const void* k, con
  *                    sequence's tokens; behind a drop, or after an eviction, see
  *                    uniprefill_append_pages_dropped
  *   num_served_dev   [1] sequences served
- * The arrays overlap in no other way.  Lengths beyond what a row of the table holds are not served; entries of the table up to a sequence's
+ * Calls that read the table, the lengths, the offsets or the slots come after this one in the stream's order
+ * (or wait for it): none may run beside it.  The arrays overlap in no other way.  Lengths beyond what a row of the table holds are not served; entries of the table up to a sequence's
  * length must name its pages.  capacity and num_seqs up to 2^31 - 65537 (UP_ERR_UNSUPPORTED),
  * kv_block_size >= 1 and block_table_stride >= 0 (UP_ERR_RANGE). */
 int uniprefill_append_pages(const int32_t* kv_len_dev, const int32_t* num_new_dev, int32_t num_seqs,

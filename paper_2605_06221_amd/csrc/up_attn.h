@@ -127,8 +127,10 @@ __device__ __forceinline__ void load_to_lds(const char* src, u32x4* dst) {
                                    (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
 }
 
-// An entry of a block table at an index that is the same for the whole wave.  No kernel writes a table, so it may come through the
-// scalar cache: its wait is then not one for the vector loads in flight.
+// An entry of a block table at an index that is the same for the whole wave, through the scalar cache: its wait is then not one for the
+// vector loads in flight.  That cache does not see what other waves write: only for kernels that leave the table alone, and while none that
+// writes it runs beside them (uniprefill_append_pages does; a call that reads the table comes after it in the stream's order, and a kernel
+// starts with a scalar cache that holds nothing older than itself).
 __device__ __forceinline__ int table_entry(const int32_t* table, unsigned i) {
   return ((const __attribute__((address_space(4))) int32_t*)table)[i];
 }

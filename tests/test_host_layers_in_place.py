@@ -1,5 +1,5 @@
-"""CPU-only tests of norm and rotation in place: an output that starts at its input with another stride, or by slots, is refused before
-anything is launched (tests/test_gpu_layers_in_place.py: rows that stay are not)."""
+"""CPU-only tests of refusals of norm and rotation: an output that starts at its input with another stride, or by slots, is refused before
+anything is launched (tests/test_gpu_layers_in_place.py: rows that stay are not), and so is what a launch cannot count."""
 import pytest
 
 import paper_2605_06221_amd as up
@@ -21,3 +21,7 @@ def _rotate(tokens=100, **kw):
 ])
 def test_moving_rows_in_place_is_refused(kw):
     assert _rotate(**kw) == up.UP_ERR_UNSUPPORTED
+
+
+def test_more_tokens_than_a_launch_has_lanes_for_are_refused():
+    assert _rotate(tokens=67108608) == up.UP_ERR_UNSUPPORTED
