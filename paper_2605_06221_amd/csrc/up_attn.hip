@@ -24,9 +24,11 @@
 // chunks on long caches by the latency of a work-group's tiles, which is why their keys are cut.
 //
 // Windowed (WINDOW): the same walk over the sinks and the band of keys that a tile's rows see, the stages that need no masks first.  A prompt of 32768,
-// window 4096 and 128 sinks: 1.97-2.05 ms, 1.04-1.08 PFLOP/s of the products that are seen (5 % more are walked over); one new token of 64
-// sequences, window 4096: 154 us, 5.2 TB/s; of one sequence, window 1024: 12 us, pieces of 128 keys and their join.  64 wide, window 1000, ragged and paged: 403 us,
-// 0.61 PFLOP/s: of 18 tiles that a work-group walks over 4 to 6 go without masks, and the others' pages are looked up lane by lane.
+// window 4096 and 128 sinks: 1.97-2.15 ms from one card to another, 0.99-1.08 PFLOP/s of the products that are seen (5 % more are walked over); one new
+// token of 64 sequences, window 4096: 154 us, 5.2 TB/s; of one sequence, window 1024: 12 us, pieces of 128 keys and their join.  64 wide, window 1000,
+// ragged and paged: 394-428 us, 0.57-0.62 PFLOP/s.  Of the 18 stages that a work-group walks over there 12 go without masks; 6 go with them, their pages
+// looked up lane by lane: the 4 at the band's ends, and 2 that are whole and left over, as the loop without masks goes in pairs and stages ahead.  The
+// masked stages of 64-wide bf16 heads read back 16 to 22 spilled registers (4 waves per SIMD leave 128).
 //
 // The weights enter the second product in bf16, their sum l in float.  Both other ways were measured, on the same inputs, as time and as
 // the output's error against 64 bits (a prompt of 32768; 46290 tokens 64 wide; 16384 tokens 256 wide), with torch in float at 1.65e-3, 1.10e-3, 1.13e-3:
@@ -478,8 +480,8 @@ __global__ __launch_bounds__(64 * WAVES, (AttnTile<F32, D, WAVES>::DENSE)) void 
     // Stages that every row sees whole lie among the sinks ([s0, s1)) and in the middle of the band ([s2, s3)); the sums do not ask for
     // an order, so these come first, as q = 0 .. n_whole - 1, and the stages that need the masks after them.  (In one loop that chose
     // between the two ways to stage, and between masks and none, the registers of the 256-wide kernel spilled 800 times, 2297 us for a
-    // prompt of 32768 with a window of 4096 against 1965; and where the branches of a stage ended in the same loads, the compiler had
-    // one of them load from an address that it had not set.)
+    // prompt of 32768 with a window of 4096 against 1965; and where the two ways of a stage ended in the same loads, the
+    // listing had one of them load from registers that nothing had set on that way; that form was never run, nor its cause found.)
     const int first = k_begin / T::KS, last = (k_end + T::KS - 1) / T::KS;
     auto within = [&](int place) { return imax(first, imin(last, place / T::KS)); };
     const int band_whole = band.sinks + imax(0, last_pos - a.window + 1 - band.low + T::KS - 1);      // (rounded up: places from here on are in every window)

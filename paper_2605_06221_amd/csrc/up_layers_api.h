@@ -49,12 +49,13 @@ int linear_args(const up_params* p, const void* q, const void* k, const void* v,
   return UP_OK;
 }
 
-// Sequences are cut into pieces of so many tokens that the batch makes a work-group for every place that the CUs have (three a CU; two where
-// the state's parts are kept in registers, one where head rows of 512 bytes fill the LDS), none shorter than two chunks.
+// Sequences are cut into pieces of so many tokens that the batch makes a work-group for every place that the CUs have (three a CU; two for 128-wide
+// heads that share a state, whose parts fill the registers; one where head rows of 512 bytes fill the LDS), none shorter than two chunks.
 // Measured, as pieces of a third, as these, as twice the size: 32768 tokens, 32/8 heads of 128, 309, 250, 270 us (two, three, four places a CU);
 // 64 wide, 40/8, ragged 184, 143, 156 (four, three, two); four and six places for all that is 64 wide: ragged 139 -> 153, 153, 32768 tokens of 32/8
 // 129 -> 132, 145, 8000 of 8/8 30 -> 37, 36, 16 x 2048 of 40/8 196 -> 184, 173.  Shortest piece of 256 and of 64 tokens: 1000 tokens, 8/8 heads of 128,
-// 34 and 23 us, 200 tokens of 32/8 heads of 64 29 and 21.
+// 34 and 23 us, 200 tokens of 32/8 heads of 64 29 and 21.  (Tokens and kv heads are all that the rule looks at.  How many query heads share a state, and
+// with it how long a piece takes, is not in it: the last of the 64-wide batches would gain 12 % from six places, where the others lose.)
 struct LinearGeometry {
   int piece;
   long long slots;

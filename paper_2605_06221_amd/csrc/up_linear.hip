@@ -101,10 +101,10 @@ __global__ __launch_bounds__(256) void k_linear_step(LinearArgs a) {
 // Long sequences are cut into pieces of `piece` tokens: one launch leaves what every piece adds to the state, a second
 // adds these up in order, and the third walks over the pieces from the states that they begin with.  Keys and values are then read twice.
 //
-// What bounds it: at one query head per kv head the bytes (a prompt of 32768, 32 heads of 128: 115 us for the first launch, 537 MB, and 230 for the
-// third, 1.07 GB, 4.7 TB/s both, 20 for the second; 410 to 430 in all), with the SIMDs full as well (matrix cores busy in 40 % of
-// the cycles, vector pipe in 63 %: most of that is taking the state apart).  With several query heads per kv head a step's own latency, about 2 us
-// from tiles to outputs, with few waves to fill it (40/8 heads of 64: matrix cores busy in 16 % of the cycles, vector pipe in 23 %): 32/8 heads 245 us.
+// What bounds it: at one query head per kv head the bytes with the SIMDs full as well (a prompt of 32768, 32 heads of 128, 407 to 440 us; its launches at
+// their fastest 126, 537 MB, and 259, 1.07 GB, both at 4.2 TB/s, and 19 for the join, with medians of 153, 311 and 21 in a profiled run; in the third
+// the matrix cores are busy in 41 % of the cycles, the vector pipe in 65 %: most of that is taking the state apart).  With several query heads per kv head a step's own latency, about 2 us
+// from tiles to outputs, with few waves to fill it (40/8 heads of 64: matrix cores busy in 16 % of the cycles, vector pipe in 23 %): 32/8 heads 231 to 255 us.
 // What it took (the same prompt): token after token 40.8 ms; chunks through registers into LDS, states scaled every chunk 490 us; two buffers and
 // one barrier a chunk 469; straight into LDS, scaled when needed, three work-groups a CU instead of two 408.  The state's parts kept
 // over the query heads, 16-byte stores and no wait for them: 32/8 heads 292 -> 259 us; eight pieces under way in the join: 8000 tokens of 8/8 heads of 64 40 -> 30.
